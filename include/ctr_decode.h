@@ -1,0 +1,152 @@
+/*
+ * ctr_decode.h -- C ABI of the operators of one decode step of a served model:
+ * what a decode instance of the simulated cluster (ctr.h) does on the KV cache
+ * that the simulator accounts for, so that the constants of its step time can
+ * be measured on the GPU that will run it.
+ *
+ *   ctr_kv_append       rotate queries and keys at their positions, append keys
+ *                       and values to a paged cache
+ *   ctr_tree_attention  attention of every sequence's new tokens (one token, a
+ *                       chain, or a tree of drafted ones) over the cache
+ *   ctr_sample          a token per row: temperature, top-k, top-p, min-p
+ *
+ * Exported by paper_2609_16206_gb300/libctr.so.  The conventions are those of
+ * ctr.h: 0 or a negative CTR_E* code, arguments validated on the host before
+ * any launch, device pointers owned by the caller, nothing allocated and no
+ * state kept between calls, work enqueued on `stream` and nothing synchronised.
+ * What only the device can see (positions, slots, lengths, page numbers) is
+ * held to its bounds by the kernels as each argument says.  The kernels are
+ * launched as programmatic dependent launches: they touch no memory before the
+ * preceding work in the stream has completed.
+ */
+#ifndef CTR_DECODE_H
+#define CTR_DECODE_H
+
+#include "ctr.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+enum ctr_dtype { CTR_BF16 = 0, CTR_F16 = 1, CTR_F32 = 2 };
+
+#define CTR_MAX_NODES 64         /* new tokens of one sequence in a ctr_tree_attention call */
+#define CTR_MAX_SEQS (1 << 14)   /* sequences of one ctr_tree_attention call */
+#define CTR_MAX_VOCAB (1 << 18)  /* logits of one row of ctr_sample */
+
+/* A paged KV cache (a host struct; CTR_BF16 or CTR_F16).  The element of page
+ * g, KV head h, token i of the page and dimension j is
+ * base[g * page_stride + h * head_stride + i * token_stride + j], the same for
+ * keys and values; strides are in elements, in any order of size.  Slot s of
+ * the cache is token s mod page_tokens of page s / page_tokens. */
+typedef struct ctr_kv_cache {
+    void* k;
+    void* v;
+    int32_t dtype;
+    int32_t n_kv_heads;   /* 1..1024 */
+    int32_t head_dim;     /* ctr_kv_append: a multiple of 8, 8..256; ctr_tree_attention: 64 or 128 */
+    int32_t page_tokens;  /* a power of two, 16..1024 */
+    int64_t n_pages;      /* 1..2^31-1 */
+    int64_t page_stride, head_stride, token_stride;
+} ctr_kv_cache;
+
+/* Rows of per-head vectors (a host struct) in the cache's dtype: element
+ * ptr[t * token_stride + h * head_stride + j]; views of a larger buffer (a
+ * fused projection's output) are what the strides are for. */
+typedef struct ctr_rows {
+    void* ptr;
+    int64_t token_stride, head_stride;
+} ctr_rows;
+
+/* Rotary positions (a host struct).  The first rot_dim elements of a head are
+ * rotated in pairs: (i, i + rot_dim / 2), or neighbours (2i, 2i + 1) where
+ * interleaved.  Pair i turns by turns[i] / 2^64 of a full turn per position, a
+ * device array of rot_dim / 2 words: the product with the position is taken
+ * modulo 2^64, so that the angle is as exact at position 2^40 as at 0, and
+ * every scaling of the frequencies for long contexts is a choice of the words.
+ * scale multiplies the rotated pairs (the attention factor of such scalings). */
+typedef struct ctr_rope {
+    const uint64_t* turns;
+    int32_t rot_dim;      /* even, 0..head_dim */
+    int32_t interleaved;  /* 0 or 1 */
+    float scale;          /* finite */
+    int32_t reserved0;    /* 0 */
+} ctr_rope;
+
+/* ctr_kv_append -- for each token t < n_tokens: q_out[t][h] = rotated q[t][h],
+ * and the rotated k[t] and the v[t] go to slot slots[t] of the cache.  With
+ * phi = 2 pi frac(positions[t] turns[i] / 2^64) a pair (x, y) becomes
+ * scale * (x cos phi - y sin phi, x sin phi + y cos phi), computed in fp32 and
+ * rounded once to the dtype; the rest of a head and all of v are copied.
+ * slots[t] < 0 (a padding row) or beyond the cache: nothing of k and v is
+ * written.  Slots must differ.  q_out may be q (with the same strides), and
+ * must not overlap it otherwise.  n_q_heads = 0 appends only.
+ * 0 <= n_tokens < 2^31, 0 <= n_q_heads <= 4096. */
+int ctr_kv_append(const ctr_kv_cache* cache /* host */, const ctr_rope* rope /* host */, ctr_rows q, ctr_rows k,
+                  ctr_rows v, ctr_rows q_out, int64_t n_tokens, int32_t n_q_heads, const int64_t* positions,
+                  const int64_t* slots, void* stream);
+
+/* ctr_attention_workspace_bytes -- device workspace ctr_tree_attention needs
+ * for these sizes on the current device (0 on bad arguments). */
+size_t ctr_attention_workspace_bytes(const ctr_kv_cache* cache /* host */, int32_t n_q_heads, int32_t n_seqs,
+                                     int32_t max_nodes);
+
+/* ctr_tree_attention -- attention of the new tokens of n_seqs sequences over a
+ * paged cache that already holds them (ctr_kv_append).  Sequence b has
+ * kv_len[b] tokens in the cache, token p in slot page_table[b * table_stride +
+ * p / page_tokens] * page_tokens + p mod page_tokens; the last
+ * T = q_start[b + 1] - q_start[b] of them are its new ones, whose queries are
+ * the rows q_start[b]..q_start[b + 1] - 1 of q.  New token i attends to all of
+ * the context (the first kv_len[b] - T tokens) and to the new tokens j with
+ * bit j of its word in tree_mask (one word per row of q) set; NULL: to new
+ * tokens 0..i (a chain).  Query head h reads KV head h / (n_q_heads /
+ * n_kv_heads).
+ *   out[t][h] = sum_p softmax_p(scale q.k_p) v_p,  lse[t * n_q_heads + h] = ln sum_p exp(scale q.k_p)
+ * over the attended p only: keys and values elsewhere, NaN and infinities
+ * among them, have no part in it.  A row that attends to nothing gives 0 and
+ * -inf.  Scores, sums and the softmax are held in fp32; the probabilities
+ * enter their product with the values in the dtype.
+ * n_q_heads a multiple of n_kv_heads, n_q_heads / n_kv_heads <= 64; 0 <= n_seqs
+ * <= CTR_MAX_SEQS; 1 <= max_nodes <= CTR_MAX_NODES: no sequence has more new
+ * tokens (those of a longer one beyond it are not computed).  kv_len[b] is held to
+ * [0, table_stride * page_tokens], rows to [0, n_rows); a page number outside
+ * the cache reads as zeros.  lse and status are optional (NULL): *status
+ * becomes CTR_ETIMEOUT where a bounded wait of the kernel ran out (never
+ * expected; the call's outputs are then unspecified).
+ * q, k, v, out: 16-byte aligned, strides multiples of 8 elements.
+ * workspace: device, 256-byte aligned, ctr_attention_workspace_bytes() or
+ * more; needs no initialisation and is clobbered. */
+int ctr_tree_attention(const ctr_kv_cache* cache /* host */, ctr_rows q, ctr_rows out, int64_t n_rows,
+                       int32_t n_q_heads, int32_t n_seqs, int32_t max_nodes, const int32_t* q_start,
+                       const int32_t* kv_len, const int32_t* page_table, int32_t table_stride,
+                       const uint64_t* tree_mask, float scale, float* lse, int32_t* status, void* workspace,
+                       size_t workspace_bytes, void* stream);
+
+/* ctr_sample -- a token per row of logits from given uniforms u in [0, 1).
+ * Every decision is an integer one, so that the token is a function of the
+ * inputs alone: a logit x (fp32 of it; NaN counts as -inf) has the weight
+ *   w = round(2^31 * 2^y),  y = max((x - max) * rate, -64),  rate = min(fl(log2 e / temperature), 3e38),
+ * with 2^y taken as 2^k P(y - k), k = y rounded to an integer and P the
+ * degree-5 polynomial of sample.cu by Horner's scheme, every fp32 step rounded
+ * on its own; a weight of 0 is never drawn.  In order of falling logits (ties:
+ * lower index first), of the tokens with a weight:
+ *   top_k[r] > 0   keeps the first top_k[r];
+ *   top_p[r] < 1   of those, the ones whose predecessors' weights sum to less
+ *                  than floor(W floor(2^31 top_p) / 2^31), W their sum, and the first;
+ *   min_p[r] > 0   of those, the ones with w >= floor(2^31 min_p);
+ * and the token is the first, in vocabulary order, at which the kept weights'
+ * running sum exceeds floor(W' floor(2^31 u) / 2^31), W' their sum.
+ * temperature[r] not > 0: the first in the order, whatever the rest says.
+ * token[r] = -1, logprob[r] = -inf, n_kept[r] = 0 where no logit is above -inf.
+ * logprob[r] = ln(w / W') of the token and n_kept[r] the number kept are
+ * optional outputs; top_k, top_p and min_p optional inputs (NULL: off; a NaN
+ * is off).  0 <= n_rows < 2^31, 1 <= vocab <= CTR_MAX_VOCAB, row_stride >= vocab. */
+int ctr_sample(const void* logits, int32_t dtype, int64_t row_stride, int64_t n_rows, int32_t vocab,
+               const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, const float* u,
+               int32_t* token, float* logprob, int32_t* n_kept, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* CTR_DECODE_H */

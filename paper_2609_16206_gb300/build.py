@@ -28,6 +28,10 @@ OBJ_CHECKED = os.path.join(HERE, "_build_checked")
 LIB_CHECKED = os.path.join(HERE, "libctr_checked.so")
 SOURCES = ["api.cu", "trace.cu", "sim.cu", "score.cu", "goodput.cu", "noalloc.cu"]
 HEADERS = [os.path.join(CSRC, "ctr_internal.cuh"), os.path.join(ROOT, "include", "ctr.h")]
+# the operators of include/ctr_decode.h: no bounds-checked variant, both libraries link the same objects
+DECODE_SOURCES = ["decode_api.cu", "kv_append.cu", "tree_attention.cu", "sample.cu"]
+DECODE_HEADERS = [os.path.join(CSRC, "decode_internal.cuh"), os.path.join(ROOT, "include", "ctr_decode.h"),
+                  os.path.join(ROOT, "include", "ctr.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 COMMON = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
           "-I", os.path.join(ROOT, "include")]
@@ -62,6 +66,13 @@ def _jobs(checked: bool, force: bool, ptxas_info: bool):
             cmd = [cc] + ARCH + COMMON + PER_FILE.get(src, []) + (["-DCTR_BOUNDS_CHECK=1"] if checked else []) + \
                   (["-Xptxas", "-v"] if ptxas_info else []) + ["-c", s, "-o", o]
             jobs.append(cmd)
+    os.makedirs(OBJ, exist_ok=True)
+    for src in DECODE_SOURCES:
+        s = os.path.join(CSRC, src)
+        o = os.path.join(OBJ, src.replace(".cu", ".o"))
+        objs.append(o)
+        if force or _stale(o, [s] + DECODE_HEADERS):
+            jobs.append([cc] + ARCH + COMMON + (["-Xptxas", "-v"] if ptxas_info else []) + ["-c", s, "-o", o])
     return jobs, objs, lib
 
 
@@ -98,7 +109,7 @@ def build_all(force: bool = False, verbose: bool = False) -> tuple:
     """libctr.so and libctr_checked.so, their translation units compiled in one pool."""
     plain = _jobs(False, force, False)
     checked = _jobs(True, force, False)
-    _run(plain[0] + checked[0], verbose, False)
+    _run(plain[0] + [job for job in checked[0] if job not in plain[0]], verbose, False)
     _link(plain[1], plain[2], force or bool(plain[0]))
     _link(checked[1], checked[2], force or bool(checked[0]))
     return plain[2], checked[2]

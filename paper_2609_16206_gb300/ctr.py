@@ -1,4 +1,4 @@
-"""ctypes binding of libctr.so (include/ctr.h).
+"""ctypes binding of libctr.so (include/ctr.h, include/ctr_decode.h).
 
 Argument marshalling only: configurations (the dataclasses of ``workloads``)
 become the C structs of ``ctr.h``; torch tensors become device pointers; the
@@ -29,6 +29,10 @@ CTR_SCORE_N_CONST = 13
 CTR_SCORE_MAX_INST = 256
 CTR_SCORE_MAX_REQ = 1 << 40
 CTR_WS_SIMULATE = 0
+CTR_BF16, CTR_F16, CTR_F32 = 0, 1, 2
+CTR_MAX_NODES = 64
+CTR_MAX_SEQS = 1 << 14
+CTR_MAX_VOCAB = 1 << 18
 
 REQUEST_FIELDS = (("arrival_us", torch.int64), ("prompt_len", torch.int32), ("true_out", torch.int32),
                   ("pred_out", torch.int32), ("slo_class", torch.uint8))
@@ -75,6 +79,22 @@ class CtrCostConsts(C.Structure):
                 ("backlog_signal", C.c_uint32), ("occupancy_poll_us", C.c_int64)]
 
 
+# ---------------------------------------------------------------- C structs (ctr_decode.h)
+class CtrKvCache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("dtype", C.c_int32), ("n_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("page_tokens", C.c_int32), ("n_pages", C.c_int64),
+                ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("token_stride", C.c_int64)]
+
+
+class CtrRows(C.Structure):
+    _fields_ = [("ptr", C.c_void_p), ("token_stride", C.c_int64), ("head_stride", C.c_int64)]
+
+
+class CtrRope(C.Structure):
+    _fields_ = [("turns", C.c_void_p), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("scale", C.c_float),
+                ("reserved0", C.c_int32)]
+
+
 _lock = threading.RLock()
 _lib = None
 
@@ -105,6 +125,16 @@ def lib():
             L.ctr_simulate_noalloc.restype = C.c_int
             L.ctr_goodput.argtypes = [C.POINTER(CtrSimCfg), CtrRequests, i32, i32, i64, vp, vp, vp, vp, vp, vp]
             L.ctr_goodput.restype = C.c_int
+            L.ctr_kv_append.argtypes = [C.POINTER(CtrKvCache), C.POINTER(CtrRope), CtrRows, CtrRows, CtrRows, CtrRows,
+                                        i64, i32, vp, vp, vp]
+            L.ctr_kv_append.restype = C.c_int
+            L.ctr_attention_workspace_bytes.argtypes = [C.POINTER(CtrKvCache), i32, i32, i32]
+            L.ctr_attention_workspace_bytes.restype = C.c_size_t
+            L.ctr_tree_attention.argtypes = [C.POINTER(CtrKvCache), CtrRows, CtrRows, i64, i32, i32, i32, vp, vp, vp,
+                                             i32, vp, C.c_float, vp, vp, vp, C.c_size_t, vp]
+            L.ctr_tree_attention.restype = C.c_int
+            L.ctr_sample.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+            L.ctr_sample.restype = C.c_int
             L.ctr_strerror.argtypes = [C.c_int]
             L.ctr_strerror.restype = C.c_char_p
             L.ctr_abi_version.restype = C.c_int
@@ -304,3 +334,108 @@ def ctr_abi_version() -> int:
 
 def ctr_bounds_checked() -> int:
     return int(lib().ctr_bounds_checked())
+
+
+# ---------------------------------------------------------------- one decode step (ctr_decode.h)
+_DTYPES = {torch.bfloat16: CTR_BF16, torch.float16: CTR_F16, torch.float32: CTR_F32}
+
+
+class KvCache:
+    """A paged KV cache: two tensors [pages, kv_heads, page_tokens, head_dim] of one 16-bit type and the same strides
+    (the last dimension contiguous; permuted views of other layouts will do).  Keeps the tensors and their C struct."""
+
+    def __init__(self, k, v):
+        if k.dtype not in (torch.bfloat16, torch.float16) or v.dtype != k.dtype:
+            raise ValueError("a KV cache is bfloat16 or float16, keys and values alike")
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.stride(3) != 1:
+            raise ValueError("expected two tensors [pages, kv_heads, page_tokens, head_dim] of the same strides, "
+                             "the last dimension contiguous")
+        if not (k.is_cuda and v.is_cuda):
+            raise ValueError("expected a CUDA tensor")
+        self.k, self.v = k, v
+        self.dtype, self.device = k.dtype, k.device
+        self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k.shape
+        self.struct = CtrKvCache(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], self.n_kv_heads, self.head_dim,
+                                 self.page_tokens, self.n_pages, k.stride(0), k.stride(1), k.stride(2))
+        self.ref = C.byref(self.struct)
+
+
+class Rope:
+    """Rotary positions of ctr_kv_append: `turns` (device int64, one word per rotated pair: the frequency in turns per
+    position times 2^64, see decode.rope_turns), the pair layout and the factor of the rotated pairs."""
+
+    def __init__(self, turns, interleaved=False, scale=1.0):
+        if turns.dtype != torch.int64 or turns.dim() != 1:
+            raise ValueError("turns must be a vector of torch.int64")
+        self.turns = turns
+        self.rot_dim = 2 * turns.numel()
+        self.struct = CtrRope(_ptr(turns), self.rot_dim, int(bool(interleaved)), float(scale), 0)
+        self.ref = C.byref(self.struct)
+
+
+def _rows(t, cache, name):
+    """[tokens, heads, head_dim] in the cache's dtype, the last dimension contiguous."""
+    if t.dim() != 3 or t.dtype != cache.dtype or t.shape[2] != cache.head_dim or not t.is_cuda or \
+            (t.stride(2) != 1 and t.numel() > 0):
+        raise ValueError(f"{name} must be a CUDA tensor [tokens, heads, {cache.head_dim}] of {cache.dtype}, the last "
+                         "dimension contiguous")
+    return CtrRows(t.data_ptr(), t.stride(0), t.stride(1))
+
+
+def _vector(t, dtype, n, name):
+    if t is None:
+        return None
+    if t.dtype != dtype or t.numel() != n:
+        raise ValueError(f"{name} must hold {n} elements of {dtype}")
+    return _ptr(t)
+
+
+def ctr_kv_append(cache: KvCache, rope: Rope, q, k, v, positions, slots, q_out, stream=None):
+    """Rotate q into q_out, append the rotated k and v to their slots.  q, k, v: [tokens, heads, head_dim]; positions
+    and slots: int64 per token (slot < 0: padding)."""
+    n = k.shape[0]
+    if k.shape != v.shape or k.dim() != 3 or k.shape[1] != cache.n_kv_heads or q.shape != q_out.shape or q.shape[0] != n:
+        raise ValueError("q, k, v and q_out must be [tokens, heads, head_dim] with the cache's heads")
+    _check("ctr_kv_append", lib().ctr_kv_append(
+        cache.ref, rope.ref, _rows(q, cache, "q"), _rows(k, cache, "k"), _rows(v, cache, "v"),
+        _rows(q_out, cache, "q_out"), n, q.shape[1], _vector(positions, torch.int64, n, "positions"),
+        _vector(slots, torch.int64, n, "slots"), _stream(stream)))
+
+
+def attention_workspace(cache: KvCache, n_q_heads: int, n_seqs: int, max_nodes: int) -> torch.Tensor:
+    n = int(lib().ctr_attention_workspace_bytes(cache.ref, int(n_q_heads), int(n_seqs), int(max_nodes)))
+    if n == 0:
+        raise CtrError("ctr_attention_workspace_bytes", CTR_EINVAL)
+    return torch.empty(n, dtype=torch.uint8, device=cache.device)
+
+
+def ctr_tree_attention(cache: KvCache, q, q_start, kv_len, page_table, out, workspace, max_nodes: int, tree_mask=None,
+                       lse=None, scale=None, status=None, stream=None):
+    """Attention of the new tokens (rows of q, sequence b's from q_start[b] to q_start[b + 1]) over the cache that holds
+    them.  q, out: [rows, heads, head_dim]; q_start int32 [n_seqs + 1]; kv_len int32 [n_seqs]; page_table int32
+    [n_seqs, width]; tree_mask int64 [rows] (bit j: attends to new token j; None: a chain); lse fp32 [rows, heads]."""
+    rows, heads = q.shape[0], q.shape[1]
+    n_seqs = kv_len.numel()
+    if out.shape != q.shape or page_table.dim() != 2 or page_table.shape[0] != n_seqs or page_table.dtype != torch.int32:
+        raise ValueError("out must have q's shape, page_table must be int32 [n_seqs, width]")
+    _check("ctr_tree_attention", lib().ctr_tree_attention(
+        cache.ref, _rows(q, cache, "q"), _rows(out, cache, "out"), rows, heads, n_seqs, int(max_nodes),
+        _vector(q_start, torch.int32, n_seqs + 1, "q_start"), _vector(kv_len, torch.int32, n_seqs, "kv_len"),
+        _ptr(page_table), page_table.shape[1], _vector(tree_mask, torch.int64, rows, "tree_mask"),
+        float(cache.head_dim ** -0.5 if scale is None else scale), _vector(lse, torch.float32, rows * heads, "lse"),
+        _vector(status, torch.int32, 1, "status"), _ptr(workspace), workspace.numel() * workspace.element_size(),
+        _stream(stream)))
+
+
+def ctr_sample(logits, temperature, u, token, top_k=None, top_p=None, min_p=None, logprob=None, n_kept=None, stream=None):
+    """A token per row of logits [rows, vocab] (bfloat16, float16 or float32, rows of any stride).  Per row: temperature,
+    u in [0, 1), top_p and min_p fp32; top_k, token and n_kept int32; logprob fp32."""
+    if logits.dim() != 2 or logits.dtype not in _DTYPES or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] > 1):
+        raise ValueError("logits must be a CUDA tensor [rows, vocab] of a floating type, the last dimension contiguous")
+    n, vocab = logits.shape
+    f32, i32 = torch.float32, torch.int32
+    _check("ctr_sample", lib().ctr_sample(
+        logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0) if n > 1 else vocab, n, vocab,
+        _vector(temperature, f32, n, "temperature"), _vector(top_k, i32, n, "top_k"), _vector(top_p, f32, n, "top_p"),
+        _vector(min_p, f32, n, "min_p"), _vector(u, f32, n, "u"), _vector(token, i32, n, "token"),
+        _vector(logprob, f32, n, "logprob"), _vector(n_kept, i32, n, "n_kept"), _stream(stream)))
