@@ -29,7 +29,8 @@ LIB_CHECKED = os.path.join(HERE, "libctr_checked.so")
 SOURCES = ["api.cu", "trace.cu", "sim.cu", "score.cu", "goodput.cu", "noalloc.cu"]
 HEADERS = [os.path.join(CSRC, "ctr_internal.cuh"), os.path.join(ROOT, "include", "ctr.h")]
 # the operators of include/ctr_decode.h: no bounds-checked variant, both libraries link the same objects
-DECODE_SOURCES = ["decode_api.cu", "kv_append.cu", "tree_attention.cu", "attention_stream.cu", "sample.cu"]
+DECODE_SOURCES = ["decode_api.cu", "kv_append.cu", "tree_attention.cu", "attention_stream.cu", "attention_tiles.cu",
+                  "sample.cu"]
 DECODE_HEADERS = [os.path.join(CSRC, "decode_internal.cuh"), os.path.join(CSRC, "attention_internal.cuh"), os.path.join(ROOT, "include", "ctr_decode.h"),
                   os.path.join(ROOT, "include", "ctr.h")]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]

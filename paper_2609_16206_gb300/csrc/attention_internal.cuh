@@ -9,27 +9,41 @@
 
 namespace ctr {
 
-constexpr unsigned kWaitLimit = 1u << 22;  // bounded mbarrier polling (a wait is a few microseconds)
+constexpr unsigned kWaitLimit = 1u << 20;  // bounded mbarrier polling (a wait is a few microseconds)
 
 // the new tokens of sequence b and its length in the cache, both held to their bounds
 struct Seq {
     int64_t row0;
     int n_new, len, context;
 };
-__device__ __forceinline__ Seq seq_of(const AttentionParams& P, int b)
+__device__ __forceinline__ Seq seq_from(const AttentionParams& P, int lo, int hi, int kv_len)
 {
     Seq s;
-    const int64_t lo = __ldg(P.q_start + b), hi = __ldg(P.q_start + b + 1);
     s.row0 = lo < 0 ? 0 : lo;
-    int64_t n = hi - lo;
-    n = n > P.max_nodes ? P.max_nodes : n;
+    const int64_t new_tokens = (int64_t)hi - lo;
+    int64_t n = new_tokens > P.max_nodes ? P.max_nodes : new_tokens;
     n = s.row0 + n > P.n_rows ? P.n_rows - s.row0 : n;
     s.n_new = n < 0 ? 0 : (int)n;
     const int64_t most = (int64_t)P.table_stride << P.page_log2;
-    const int64_t len = __ldg(P.kv_len + b);
-    s.len = len < 0 ? 0 : len > most ? (int)most : (int)len;
-    s.context = s.len - (int)(hi - lo);
+    s.len = kv_len < 0 ? 0 : kv_len > most ? (int)most : kv_len;
+    s.context = s.len - (int)new_tokens;
     return s;
+}
+__device__ __forceinline__ Seq seq_of(const AttentionParams& P, int b)
+{
+    return seq_from(P, __ldg(P.q_start + b), __ldg(P.q_start + b + 1), __ldg(P.kv_len + b));
+}
+
+__device__ __forceinline__ int node_of(const AttentionParams& P, int r) { return (int)((uint32_t)r * P.group_magic >> 20); }
+
+// Which of the (at most 32) tokens from `key` on a new token with mask `mask` attends to, a bit each.
+__device__ __forceinline__ uint32_t seen_tokens(const Seq& s, uint64_t mask, int key)
+{
+    const int before = s.context - key, end = s.len - key;  // tokens of the context, tokens there are
+    const uint32_t all = end >= 32 ? ~0u : (1u << end) - 1u;
+    if (before >= 32) return all;
+    if (before > 0) return ((uint32_t)(mask << before) | ((1u << before) - 1u)) & all;
+    return before > -64 ? (uint32_t)(mask >> -before) & all : 0u;
 }
 
 // ---------------------------------------------------------------- shared memory, mbarriers, TMA
@@ -77,34 +91,53 @@ __device__ __forceinline__ float exp2_fast(float x)
 }
 
 // ---------------------------------------------------------------- the split of the work
-// A sequence's KV head is an item of ceil(len / kUnit) units, one at least; the units of all items, in order, are cut
-// into equal ranges, one a block.  A range holds whole items and at most two parts of items, its first and last;
-// such a part leaves its sums in the block's first (an item begun by an earlier block) or second slot of the
-// workspace, and the merge kernel joins the slots of an item in the order of its blocks.
+// A sequence's KV head is an item of ceil(len / unit) units, one at least, or several such items where its query rows
+// (group x new tokens) are more than the item_rows that a block takes.  Items cost kUnitCost a unit and kItemCost
+// for their begin and end, in half units of time; the cost of all items, in order, is cut into equal ranges, one a
+// block, and a cut inside an item goes to the unit that it falls in.  A range holds whole items and at most two parts
+// of items, its first and last; such a part leaves its sums in the block's first (an item begun by an earlier block)
+// or second slot of the workspace, and the merge kernel joins the slots of an item in the order of its blocks.
+constexpr int kUnitCost = 2, kItemCost = 1;
+
 struct SplitSlot {           // the item that a block begins and does not end
-    int32_t b, h, last;      // sequence (-1: none), KV head, the block that ends it
-    int32_t reserved;
+    int32_t b, h, row0, last;  // sequence (-1: none), KV head, first row, the block that ends it
 };
 
-template <int kUnit>
-__device__ __forceinline__ int64_t units_of(const Seq& s)
+__device__ __forceinline__ int units_of(const Seq& s, int unit)
 {
-    return s.n_new == 0 ? 0 : s.len <= kUnit ? 1 : (s.len + kUnit - 1) / kUnit;
+    return s.n_new == 0 ? 0 : s.len <= unit ? 1 : (s.len + unit - 1) / unit;
+}
+__device__ __forceinline__ int64_t cost_of(int units) { return units == 0 ? 0 : (int64_t)kUnitCost * units + kItemCost; }
+// the unit of an item that a cut `off` into its cost falls in
+__device__ __forceinline__ int unit_at(int64_t off) { return off <= kItemCost ? 0 : (int)((off - kItemCost) / kUnitCost); }
+
+__device__ __forceinline__ int items_of(const AttentionParams& P, const Seq& s, int item_rows)
+{
+    const int rows = s.n_new * P.group;
+    return P.cache.n_kv_heads * (rows <= item_rows ? 1 : (rows + item_rows - 1) / item_rows);
 }
 
-// The range of block c: `count` units from unit `begin` of `total` on, which is unit `within` of sequence b0 (over
-// all of its KV heads); `blocks`, the grid's on entry, becomes the number of blocks with work, each of which has a
-// unit at least.  By all threads of the block; scratch: kThreads / 32 + 4 words of 64 bits.
-template <int kUnit, int kThreads>
-__device__ void find_range(const AttentionParams& P, int c, int64_t* scratch, int& blocks, int64_t& total, int64_t& begin,
-                           int64_t& count, int& b0, int64_t& within)
+struct Range {
+    int64_t begin, end, total;  // of the cost
+    int blocks;                 // with work: each has a unit at least
+    int b;                      // the sequence that it begins in, and where in it (over its KV heads)
+    int64_t within;
+};
+
+// The range of block c; by all threads of the block.  scratch: kThreads / 32 + 2 words of 64 bits.
+template <int kThreads>
+__device__ Range find_range(const AttentionParams& P, int unit, int item_rows, int c, int blocks, int64_t* scratch)
 {
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const int per = (P.n_seqs + kThreads - 1) / kThreads;
     const int first = min(tid * per, P.n_seqs), last = min(first + per, P.n_seqs);
+    auto cost_at = [&](int b) {
+        const Seq s = seq_of(P, b);
+        return cost_of(units_of(s, unit)) * items_of(P, s, item_rows);
+    };
     int64_t mine = 0;
-    for (int b = first; b < last; ++b) mine += units_of<kUnit>(seq_of(P, b)) * P.cache.n_kv_heads;
+    for (int b = first; b < last; ++b) mine += cost_at(b);
     int64_t sum = mine;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
@@ -113,40 +146,96 @@ __device__ void find_range(const AttentionParams& P, int c, int64_t* scratch, in
     }
     if (lane == 31) scratch[wid] = sum;
     __syncthreads();
-    int64_t all = 0;
+    Range r;
+    r.total = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-        if (w == wid) sum += all;
-        all += scratch[w];
+        if (w == wid) sum += r.total;
+        r.total += scratch[w];
     }
-    total = all;
-    if (all < blocks) blocks = (int)all;
-    count = 0;
-    if (c >= blocks) return;  // the whole block
-    begin = all * c / blocks;
-    count = all * (c + 1) / blocks - begin;
+    r.blocks = (int)min((int64_t)blocks, r.total / (kUnitCost + kItemCost));
+    r.begin = r.end = r.within = 0;
+    r.b = 0;
+    if (c >= r.blocks) return r;  // the whole block
+    r.begin = r.total * c / r.blocks;
+    r.end = r.total * (c + 1) / r.blocks;
     int64_t at = sum - mine;
-    if (at <= begin && begin < sum) {
+    if (at <= r.begin && r.begin < sum) {
         for (int b = first; b < last; ++b) {
-            const int64_t n = units_of<kUnit>(seq_of(P, b)) * P.cache.n_kv_heads;
-            if (begin < at + n) {
+            const int64_t n = cost_at(b);
+            if (r.begin < at + n) {
                 scratch[kWarps] = b;
-                scratch[kWarps + 1] = begin - at;
+                scratch[kWarps + 1] = r.begin - at;
                 break;
             }
             at += n;
         }
     }
     __syncthreads();
-    b0 = (int)scratch[kWarps];
-    within = scratch[kWarps + 1];
+    r.b = (int)scratch[kWarps];
+    r.within = scratch[kWarps + 1];
+    return r;
 }
 
-// the block whose range holds unit u: the largest c with floor(total c / blocks) <= u (blocks <= total)
-__device__ __forceinline__ int block_of(int64_t u, int64_t total, int blocks)
-{
-    return (int)(((u + 1) * blocks - 1) / total);
-}
+// A block's way through its range: the items in order (h: of the sequence) and of each the units [u, end).
+struct Walk {
+    Seq s;
+    int b, h, u, begin, end, units, items;
+    int64_t left;              // of the range's cost, from the item's begin on
+    int raw_lo, raw_hi, raw_len;  // the next sequence's bounds, loaded ahead
+
+    __device__ __forceinline__ void load_ahead(const AttentionParams& P)
+    {
+        const int n = b + 1 < P.n_seqs ? b + 1 : b;
+        raw_lo = __ldg(P.q_start + n);
+        raw_hi = __ldg(P.q_start + n + 1);
+        raw_len = __ldg(P.kv_len + n);
+    }
+    __device__ __forceinline__ void enter(int64_t off)
+    {
+        begin = u = unit_at(off);
+        end = min(units, unit_at(left));
+    }
+    __device__ __forceinline__ bool more() const { return left > 0 && end > 0; }
+    __device__ __forceinline__ void start(const AttentionParams& P, const Range& r, int unit, int item_rows)
+    {
+        b = r.b;
+        left = r.end - r.begin;
+        end = 0;
+        if (left <= 0) return;
+        s = seq_of(P, b);
+        units = units_of(s, unit);
+        items = items_of(P, s, item_rows);
+        const int64_t cost = cost_of(units);
+        h = (int)(r.within / cost);
+        const int64_t off = r.within - h * cost;
+        left += off;
+        enter(off);
+        load_ahead(P);
+    }
+    __device__ __forceinline__ void next(const AttentionParams& P, int unit, int item_rows)
+    {
+        left -= cost_of(units);
+        if (left <= 0) return;
+        if (++h == items) {
+            h = 0;
+            do {
+                ++b;
+                s = seq_from(P, raw_lo, raw_hi, raw_len);
+                units = units_of(s, unit);
+                load_ahead(P);
+            } while (units == 0);
+            items = items_of(P, s, item_rows);
+        }
+        enter(0);
+    }
+    // the block that ends the item, which this range begins at cost `range_end - left`
+    __device__ __forceinline__ int last_block(const Range& r) const
+    {
+        const int64_t pos = r.end - left + kItemCost + (int64_t)kUnitCost * units - 1;
+        return (int)(((pos + 1) * r.blocks - 1) / r.total);  // the largest c with floor(total c / blocks) <= pos
+    }
+};
 
 // Workspace: blocks SplitSlots, then per block and slot the partial sums of up to `rows` rows: their maxima and
 // weight sums, and `rows` x head_dim fp32 outputs.
@@ -161,7 +250,10 @@ __device__ __forceinline__ float* part_of_item(const AttentionParams& P, int blo
 cudaError_t make_cache_maps(const AttentionParams& p, int box_tokens, CUtensorMap* k, CUtensorMap* v);
 cudaError_t launch_merge(const AttentionParams& p, int blocks, int rows, cudaStream_t stream);
 
-int stream_blocks();  // of the kernel for few rows a KV head
+int sm_count();  // of the current device
+size_t stream_workspace(int rows, int d);
+size_t tiles_workspace(int rows, int d);
+cudaError_t launch_tiles(const AttentionParams& p, cudaStream_t stream);  // more than 32 rows a KV head
 cudaError_t launch_stream(const AttentionParams& p, cudaStream_t stream);
 
 }  // namespace ctr

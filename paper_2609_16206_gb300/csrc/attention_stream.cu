@@ -16,10 +16,6 @@ namespace ctr {
 namespace {
 
 constexpr int kWarps = 4, kThreads = 32 * kWarps;
-constexpr int kChunk = 16;               // tokens of a chunk
-constexpr int kUnit = kWarps * kChunk;   // tokens of a unit of work
-constexpr int kStages = 3;
-constexpr int kBlocksPerSm = 2;
 
 template <typename T> struct Mma;
 template <> struct Mma<__nv_bfloat16> {
@@ -56,67 +52,40 @@ __device__ __forceinline__ void ldsm4_trans(uint32_t (&r)[4], uint32_t addr)
                  : "memory");
 }
 
-// byte offset of 16-byte piece `c` (of 8 * D / 64) of token `r` in a chunk of keys or values: halves of 64
-// dimensions, 128-byte rows, pieces swizzled by the row as TMA leaves them
-__device__ __forceinline__ uint32_t piece(int r, int c)
-{
-    return (uint32_t)((c >> 3) * (kChunk * 128) + r * 128 + (((c & 7) ^ (r & 7)) << 4));
-}
-
-// The sequence of chunks of a warp: items in order, of each the units in the block's range.
-struct Walk {
-    Seq s;
-    int b, h, u, end;   // the item's current unit and the end of its part in this range
-    int units;
-    int64_t left;       // units of the range from this part on
-
-    __device__ __forceinline__ void start(const AttentionParams& P, int b0, int64_t within, int64_t count)
-    {
-        b = b0;
-        left = count;
-        if (left <= 0) return;
-        s = seq_of(P, b);
-        units = (int)units_of<kUnit>(s);
-        h = (int)(within / units);
-        u = (int)(within - (int64_t)h * units);
-        end = left < units - u ? u + (int)left : units;
-    }
-    // to the next item (u has reached end)
-    __device__ __forceinline__ void next(const AttentionParams& P, int begin)
-    {
-        left -= end - begin;
-        u = 0;
-        if (left <= 0) return;
-        if (++h == P.cache.n_kv_heads) {
-            h = 0;
-            do {
-                s = seq_of(P, ++b);
-                units = (int)units_of<kUnit>(s);
-            } while (units == 0);
-        }
-        end = left < units ? (int)left : units;
-    }
-};
-
+// Chunks of 8 KB whatever the head, so that 64-wide heads have the same work between two waits.  Blocks per SM by the
+// registers of the accumulators (16 rows x D of fp32 a warp, kTiles of them); stages by the shared memory left.
 template <int D, int kTiles>
 struct Layout {
     static constexpr int kRows = 16 * kTiles;
+    static constexpr int kSub = 128 / D;                      // groups of 16 tokens of a chunk
+    static constexpr int kChunk = 16 * kSub;                  // tokens of a chunk
+    static constexpr int kUnit = kWarps * kChunk;             // tokens of a unit of work
+    static constexpr int kBlocksPerSm = 2;
+    static constexpr int kStages = 3;
     static constexpr int kHalf = kChunk * 128;                // bytes of 64 dimensions of a chunk
     static constexpr int kStage = 2 * (D / 64) * kHalf;       // keys, then values
     static constexpr int kRing = kWarps * kStages * kStage;
-    static constexpr int kJoin = kRing;                       // float [kWarps][8][D]
-    static constexpr int kStats = kJoin + kWarps * 8 * D * 4; // float [kWarps][8] maxima, then sums
+    static constexpr int kJoin = kRing;                       // float [kWarps][8][64]
+    static constexpr int kStats = kJoin + kWarps * 8 * 64 * 4; // float [kWarps][8] maxima, then sums
     static constexpr int kScratch = kStats + kWarps * 8 * 8;
-    static constexpr int kBars = kScratch + (kWarps + 4) * 8;
+    static constexpr int kBars = kScratch + (kWarps + 2) * 8;
     static constexpr int kBytes = kBars + kWarps * kStages * 8;
+
+    // byte offset of 16-byte piece `c` (of D / 8) of token `r` in a chunk of keys or values: halves of 64 dimensions,
+    // 128-byte rows, pieces swizzled by the row as TMA leaves them
+    static __device__ __forceinline__ uint32_t piece(int r, int c)
+    {
+        return (uint32_t)((c >> 3) * kHalf + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+    }
 };
 
 template <typename T, int D, int kTiles>
-__global__ void __launch_bounds__(kThreads, kBlocksPerSm)
+__global__ void __launch_bounds__(kThreads, (Layout<D, kTiles>::kBlocksPerSm))
 stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttentionParams P)
 {
     using L = Layout<D, kTiles>;
     constexpr int kN = D / 8;  // 8-wide tiles of the output
+    constexpr int kSub = L::kSub, kChunk = L::kChunk, kUnit = L::kUnit, kStages = L::kStages;
     extern __shared__ __align__(1024) unsigned char smem[];
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5, g = lane >> 2, t = lane & 3;
     const uint32_t ring = smem_u32(smem) + wid * kStages * L::kStage;
@@ -130,48 +99,47 @@ stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
     __syncwarp();
     wait_for_previous_kernels();
 
-    int64_t total, begin, count, within;
-    int b0, blocks = gridDim.x;  // with work
-    find_range<kUnit, kThreads>(P, blockIdx.x, reinterpret_cast<int64_t*>(smem + L::kScratch), blocks, total, begin, count, b0, within);
+    const Range range = find_range<kThreads>(P, kUnit, L::kRows, blockIdx.x, gridDim.x, reinterpret_cast<int64_t*>(smem + L::kScratch));
     if (tid == 0) split_slots(P)[blockIdx.x].b = -1;
-    if (count <= 0) return;
+    if (range.end <= range.begin) return;
 
     Walk make, take;  // the chunks to load and the ones to compute on
-    make.start(P, b0, within, count);
+    make.start(P, range, kUnit, L::kRows);
     take = make;
 
-    // page numbers of the next 32 chunks to load, one a lane
-    int pages = 0, pages_at = 0, pages_n = 0, make_begin = make.u;
-    uint32_t made = 0, taken = 0;
+    // page numbers of the next 32 / kSub chunks to load, one for each group of 16 tokens (-1: past the end, reads zeros)
+    int pages = 0, pages_at = 32;
+    uint32_t made = 0, taken = 0, make_stage = 0, take_stage = 0, take_phase = 0;
     bool fine = true;
     auto load_next = [&]() {  // issues the next chunk there is
-        while (fine && make.left > 0) {
+        while (fine && make.more()) {
             const int key = make.u * kUnit + wid * kChunk;
             if (make.u >= make.end || key >= make.s.len) {  // this warp's part of the item is through
-                make.u = make.end;
-                make.next(P, make_begin);
-                make_begin = make.u;
-                pages_n = 0;
+                make.next(P, kUnit, L::kRows);
+                pages_at = 32;
                 continue;
             }
-            if (pages_n == 0) {
-                const int k = key + lane * kUnit;
-                pages = k < make.s.len ? __ldg(P.page_table + (int64_t)make.b * P.table_stride + (k >> P.page_log2)) : 0;
+            if (pages_at == 32) {
+                const int k = key + lane / kSub * kUnit + lane % kSub * 16;
+                pages = k < make.s.len ? __ldg(P.page_table + (int64_t)make.b * P.table_stride + (k >> P.page_log2)) : -1;
                 pages_at = 0;
-                pages_n = 32;
             }
-            const int page = __shfl_sync(~0u, pages, pages_at++);
-            --pages_n;
-            if (lane == 0) {
-                const uint32_t stage = made % kStages, bar = bars + 8 * stage, dst = ring + stage * L::kStage;
-                const int y = key & (P.cache.page_tokens - 1);
-                bar_expect(bar, L::kStage);
+            const uint32_t bar = bars + 8 * make_stage, dst = ring + make_stage * L::kStage;
+            make_stage = make_stage + 1 == kStages ? 0 : make_stage + 1;
 #pragma unroll
-                for (int i = 0; i < D / 64; ++i) {
-                    tma_load(dst + i * L::kHalf, &map_k, bar, 64 * i, y, make.h, page);
-                    tma_load(dst + (D / 64 + i) * L::kHalf, &map_v, bar, 64 * i, y, make.h, page);
+            for (int j = 0; j < kSub; ++j) {
+                const int page = __shfl_sync(~0u, pages, pages_at + j);
+                if (lane == 0) {
+                    const int y = (key + 16 * j) & (P.cache.page_tokens - 1);
+                    if (j == 0) bar_expect(bar, L::kStage);
+#pragma unroll
+                    for (int i = 0; i < D / 64; ++i) {
+                        tma_load(dst + i * L::kHalf + j * 2048, &map_k, bar, 64 * i, y, make.h, page);
+                        tma_load(dst + (D / 64 + i) * L::kHalf + j * 2048, &map_v, bar, 64 * i, y, make.h, page);
+                    }
                 }
             }
+            pages_at += kSub;
             ++made;
             ++make.u;
             return;
@@ -180,9 +148,9 @@ stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
 #pragma unroll 1
     for (int i = 0; i < kStages; ++i) load_next();
 
-    while (take.left > 0) {
+    while (take.more()) {
         // the item's queries as A operands: row r of the item is new token r / group, query head h * group + r % group
-        const int rows = take.s.n_new * P.group, part_begin = take.u;
+        const int rows = take.s.n_new * P.group;
         uint32_t q[kTiles][D / 16][4];
         uint64_t mask[kTiles][2];
 #pragma unroll
@@ -191,7 +159,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
             for (int i = 0; i < 2; ++i) {
                 const int r = 16 * m + 8 * i + g;
                 const bool is = r < rows;
-                const int node = is ? r / P.group : 0;
+                const int node = is ? node_of(P, r) : 0;
                 const int64_t row = take.s.row0 + node;
                 const T* src = static_cast<const T*>(P.q.ptr) + row * P.q.token_stride +
                                (int64_t)(take.h * P.group + r - node * P.group) * P.q.head_stride;
@@ -215,8 +183,8 @@ stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
         for (; take.u < take.end; ++take.u) {
             const int key = take.u * kUnit + wid * kChunk;
             if (key >= take.s.len || !fine) continue;
-            const uint32_t stage = taken % kStages, base = ring + stage * L::kStage, vbase = base + L::kStage / 2;
-            if (!bar_wait(bars + 8 * stage, (taken / kStages) & 1)) {
+            const uint32_t base = ring + take_stage * L::kStage, vbase = base + L::kStage / 2;
+            if (!bar_wait(bars + 8 * take_stage, take_phase)) {
                 // never expected: report it, give every load in flight a second bounded wait (they must not outlive the
                 // block's shared memory), load and compute no more
                 fine = false;
@@ -225,40 +193,52 @@ stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                 continue;
             }
             ++taken;
+            if (++take_stage == kStages) {
+                take_stage = 0;
+                take_phase ^= 1;
+            }
 
-            float s[kTiles][2][4];
+            float s[kTiles][2 * kSub][4];
 #pragma unroll
             for (int m = 0; m < kTiles; ++m)
 #pragma unroll
-                for (int n = 0; n < 2; ++n) s[m][n][0] = s[m][n][1] = s[m][n][2] = s[m][n][3] = 0.f;
+                for (int n = 0; n < 2 * kSub; ++n) s[m][n][0] = s[m][n][1] = s[m][n][2] = s[m][n][3] = 0.f;
 #pragma unroll
             for (int k = 0; k < D / 16; ++k) {
-                uint32_t kb[4];  // dimensions 0-7 and 8-15 of tokens 0-7, then of tokens 8-15
-                ldsm4(kb, base + piece((lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
 #pragma unroll
-                for (int m = 0; m < kTiles; ++m) {
-                    Mma<T>::run(s[m][0], q[m][k], kb[0], kb[1]);
-                    Mma<T>::run(s[m][1], q[m][k], kb[2], kb[3]);
+                for (int j = 0; j < kSub; ++j) {
+                    uint32_t kb[4];  // dimensions 0-7 and 8-15 of tokens 0-7, then of tokens 8-15
+                    ldsm4(kb, base + L::piece(16 * j + (lane & 7) + ((lane >> 4) << 3), 2 * k + ((lane >> 3) & 1)));
+#pragma unroll
+                    for (int m = 0; m < kTiles; ++m) {
+                        Mma<T>::run(s[m][2 * j], q[m][k], kb[0], kb[1]);
+                        Mma<T>::run(s[m][2 * j + 1], q[m][k], kb[2], kb[3]);
+                    }
                 }
             }
             const bool edge = key + kChunk > take.s.context;  // new tokens, or the end
 #pragma unroll
             for (int m = 0; m < kTiles; ++m) {
 #pragma unroll
-                for (int n = 0; n < 2; ++n)
+                for (int n = 0; n < 2 * kSub; ++n)
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        float x = s[m][n][e] * P.scale_log2;
-                        if (edge) {
-                            const int p = key + 8 * n + 2 * t + (e & 1), node = p - take.s.context;
-                            const bool seen = p < take.s.len && (node < 0 || (mask[m][e >> 1] >> node & 1));
-                            x = seen ? x : -INFINITY;
-                        }
-                        s[m][n][e] = x;
+                    for (int e = 0; e < 4; ++e) s[m][n][e] *= P.scale_log2;
+                if (edge) {
+#pragma unroll
+                    for (int i = 0; i < 2; ++i) {
+                        const uint32_t seen = seen_tokens(take.s, mask[m][i], key) >> 2 * t;
+#pragma unroll
+                        for (int n = 0; n < 2 * kSub; ++n)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e)
+                                if (!(seen >> (8 * n + e) & 1)) s[m][n][2 * i + e] = -INFINITY;
                     }
+                }
 #pragma unroll
                 for (int i = 0; i < 2; ++i) {
-                    float x = fmaxf(fmaxf(s[m][0][2 * i], s[m][0][2 * i + 1]), fmaxf(s[m][1][2 * i], s[m][1][2 * i + 1]));
+                    float x = -INFINITY;
+#pragma unroll
+                    for (int n = 0; n < 2 * kSub; ++n) x = fmaxf(x, fmaxf(s[m][n][2 * i], s[m][n][2 * i + 1]));
                     x = fmaxf(x, __shfl_xor_sync(~0u, x, 1));
                     x = fmaxf(x, __shfl_xor_sync(~0u, x, 2)) - Mma<T>::kLift;
                     if (x > top[m][i]) {  // the maxima settle after a few chunks: most pass this by
@@ -273,7 +253,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                     }
                     const float ref = top[m][i] == -INFINITY ? 0.f : top[m][i];
 #pragma unroll
-                    for (int n = 0; n < 2; ++n)
+                    for (int n = 0; n < 2 * kSub; ++n)
 #pragma unroll
                         for (int e = 2 * i; e < 2 * i + 2; ++e) {
                             s[m][n][e] = exp2_fast(s[m][n][e] - ref);
@@ -284,71 +264,74 @@ stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
             if (edge) {
                 // Values that no row may see, or only some: those past the end become zeros, and a new token's that is
                 // not finite is added here, to the rows that attend to it, and kept out of the product.
-                const int r = lane & 15, p = key + r, node = p - take.s.context;
-                bool bad = false;
-                for (int c = lane >> 4; c < D / 8; c += 2) {
-                    const uint4 v = *reinterpret_cast<const uint4*>(smem + (vbase - smem_u32(smem)) + piece(r, c));
-                    const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+                unsigned char* values = smem + (vbase - smem_u32(smem));
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const float2 f = Pair<T>::split(w[i]);
-                        bad = bad || !(fabsf(f.x) < INFINITY) || !(fabsf(f.y) < INFINITY);
+                for (int j = 0; j < kSub; ++j) {
+                    const int r = lane & 15, p = key + 16 * j + r, node = p - take.s.context;
+                    uint32_t bad = 0;
+#pragma unroll 4
+                    for (int c = lane >> 4; c < D / 8; c += 2) {
+                        const uint4 v = *reinterpret_cast<const uint4*>(values + L::piece(16 * j + r, c));
+                        bad |= not_finite<T>(v.x) | not_finite<T>(v.y) | not_finite<T>(v.z) | not_finite<T>(v.w);
                     }
-                }
-                uint32_t clear = __ballot_sync(~0u, bad && node >= 0 && p < take.s.len);
-                clear = (clear | clear >> 16) & 0xffffu;
-                for (uint32_t todo = clear; todo; todo &= todo - 1) {
-                    const int k = __ffs(todo) - 1, n = key + k - take.s.context;
+                    uint32_t clear = __ballot_sync(~0u, bad && node >= 0 && p < take.s.len);
+                    clear = (clear | clear >> 16) & 0xffffu;
+                    for (uint32_t todo = clear; __builtin_expect(todo != 0, 0); todo &= todo - 1) {
+                        const int k = __ffs(todo) - 1, n = key + 16 * j + k - take.s.context;
 #pragma unroll
-                    for (int m = 0; m < kTiles; ++m)
+                        for (int m = 0; m < kTiles; ++m)
 #pragma unroll
-                        for (int i = 0; i < 2; ++i) {
-                            const float mine = k < 8 ? (k & 1 ? s[m][0][2 * i + 1] : s[m][0][2 * i]) : (k & 1 ? s[m][1][2 * i + 1] : s[m][1][2 * i]);
-                            const float w = __shfl_sync(~0u, mine, (lane & 28) + ((k & 7) >> 1));
-                            if (mask[m][i] >> n & 1)
+                            for (int i = 0; i < 2; ++i) {
+                                const float lo = k & 1 ? s[m][2 * j][2 * i + 1] : s[m][2 * j][2 * i];
+                                const float hi = k & 1 ? s[m][2 * j + 1][2 * i + 1] : s[m][2 * j + 1][2 * i];
+                                const float w = __shfl_sync(~0u, k < 8 ? lo : hi, (lane & 28) + ((k & 7) >> 1));
+                                if (mask[m][i] >> n & 1)
 #pragma unroll
-                                for (int j = 0; j < kN; ++j) {
-                                    const uint32_t v = *reinterpret_cast<const uint32_t*>(smem + (vbase - smem_u32(smem)) + piece(k, j) + 4 * t);
-                                    const float2 f = Pair<T>::split(v);
-                                    o[m][j][2 * i] += w * f.x;
-                                    o[m][j][2 * i + 1] += w * f.y;
-                                }
-                        }
-                }
-                __syncwarp();
-                if (p >= take.s.len || (clear >> r & 1)) {
-                    for (int c = lane >> 4; c < D / 8; c += 2)
-                        *reinterpret_cast<uint4*>(smem + (vbase - smem_u32(smem)) + piece(r, c)) = make_uint4(0, 0, 0, 0);
+                                    for (int d = 0; d < kN; ++d) {
+                                        const uint32_t v = *reinterpret_cast<const uint32_t*>(values + L::piece(16 * j + k, d) + 4 * t);
+                                        const float2 f = Pair<T>::split(v);
+                                        o[m][d][2 * i] += w * f.x;
+                                        o[m][d][2 * i + 1] += w * f.y;
+                                    }
+                            }
+                    }
+                    __syncwarp();
+                    if (p >= take.s.len || (clear >> r & 1)) {
+                        for (int c = lane >> 4; c < D / 8; c += 2)
+                            *reinterpret_cast<uint4*>(values + L::piece(16 * j + r, c)) = make_uint4(0, 0, 0, 0);
+                    }
                 }
                 asm volatile("fence.proxy.async.shared::cta;" ::: "memory");  // before the stage's next load
                 __syncwarp();
             }
-            uint32_t pr[kTiles][4];
 #pragma unroll
-            for (int m = 0; m < kTiles; ++m) {
-                pr[m][0] = Pair<T>::join(s[m][0][0], s[m][0][1]);
-                pr[m][1] = Pair<T>::join(s[m][0][2], s[m][0][3]);
-                pr[m][2] = Pair<T>::join(s[m][1][0], s[m][1][1]);
-                pr[m][3] = Pair<T>::join(s[m][1][2], s[m][1][3]);
-            }
-#pragma unroll
-            for (int n = 0; n < kN; n += 2) {
-                uint32_t vb[4];  // tokens 0-7 and 8-15 of one tile of dimensions, then of the next
-                ldsm4_trans(vb, vbase + piece((lane & 7) + (((lane >> 3) & 1) << 3), n + (lane >> 4)));
+            for (int j = 0; j < kSub; ++j) {
+                uint32_t pr[kTiles][4];
 #pragma unroll
                 for (int m = 0; m < kTiles; ++m) {
-                    Mma<T>::run(o[m][n], pr[m], vb[0], vb[1]);
-                    Mma<T>::run(o[m][n + 1], pr[m], vb[2], vb[3]);
+                    pr[m][0] = Pair<T>::join(s[m][2 * j][0], s[m][2 * j][1]);
+                    pr[m][1] = Pair<T>::join(s[m][2 * j][2], s[m][2 * j][3]);
+                    pr[m][2] = Pair<T>::join(s[m][2 * j + 1][0], s[m][2 * j + 1][1]);
+                    pr[m][3] = Pair<T>::join(s[m][2 * j + 1][2], s[m][2 * j + 1][3]);
+                }
+#pragma unroll
+                for (int n = 0; n < kN; n += 2) {
+                    uint32_t vb[4];  // tokens 0-7 and 8-15 of one tile of dimensions, then of the next
+                    ldsm4_trans(vb, vbase + L::piece(16 * j + (lane & 7) + (((lane >> 3) & 1) << 3), n + (lane >> 4)));
+#pragma unroll
+                    for (int m = 0; m < kTiles; ++m) {
+                        Mma<T>::run(o[m][n], pr[m], vb[0], vb[1]);
+                        Mma<T>::run(o[m][n + 1], pr[m], vb[2], vb[3]);
+                    }
                 }
             }
             __syncwarp();
             load_next();
         }
 
-        // The four warps' sums: maxima and weights first, then the outputs, eight rows at a time.
-        const bool whole = part_begin == 0 && take.end == take.units;
-        const int slot = part_begin == 0 ? 1 : 0;
-        float* part = part_of_item(P, gridDim.x, L::kRows, D, blockIdx.x, slot);
+        // The four warps' sums: maxima and weights, then the outputs, eight rows x 64 dimensions at a time.
+        const bool whole = take.begin == 0 && take.end == take.units;
+        float* part = part_of_item(P, gridDim.x, L::kRows, D, blockIdx.x, take.begin == 0 ? 1 : 0);
         float* join = reinterpret_cast<float*>(smem + L::kJoin);
         float* stat = reinterpret_cast<float*>(smem + L::kStats);
 #pragma unroll
@@ -369,62 +352,62 @@ stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
 #pragma unroll
                 for (int w = 0; w < kWarps; ++w) most = fmaxf(most, stat[w * 8 + g]);
                 const float fix = top[m][i] == -INFINITY ? 0.f : exp2_fast(top[m][i] - most);
+                const int r = tid >> 4, c = tid & 15;  // this thread's row and 4 of its 64 dimensions
+                float lsum = 0.f, high = -INFINITY;
 #pragma unroll
-                for (int n = 0; n < kN; ++n) {
-                    float2* at = reinterpret_cast<float2*>(join + (wid * 8 + g) * D + ((8 * n + 2 * t) ^ (8 * (g & 3))));
-                    *at = make_float2(o[m][n][2 * i] * fix, o[m][n][2 * i + 1] * fix);
+                for (int w = 0; w < kWarps; ++w) high = fmaxf(high, stat[w * 8 + r]);
+#pragma unroll
+                for (int w = 0; w < kWarps; ++w) {
+                    const float mw = stat[w * 8 + r];
+                    lsum += mw == -INFINITY ? 0.f : exp2_fast(mw - high) * stat[(kWarps + w) * 8 + r];
                 }
-                __syncthreads();
-                constexpr int kCols = D / 8;
-                const int r = tid / kCols, c = tid % kCols;
-                if (r < 8 && r0 + r < rows) {
-                    float x[8], lsum = 0.f, high = -INFINITY;
+                const int node = node_of(P, r0 + r);
+                const int64_t row = take.s.row0 + node, head = take.h * P.group + r0 + r - node * P.group;
+                const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[e] = 0.f;
+                for (int half = 0; half < D / 64; ++half) {
 #pragma unroll
-                    for (int w = 0; w < kWarps; ++w) high = fmaxf(high, stat[w * 8 + r]);
-#pragma unroll
-                    for (int w = 0; w < kWarps; ++w) {
-                        const float mw = stat[w * 8 + r];
-                        lsum += mw == -INFINITY ? 0.f : exp2_fast(mw - high) * stat[(kWarps + w) * 8 + r];
-                        const float4* from = reinterpret_cast<const float4*>(join + (w * 8 + r) * D + ((8 * c) ^ (8 * (r & 3))));
-                        const float4 v0 = from[0], v1 = from[1];
-                        x[0] += v0.x, x[1] += v0.y, x[2] += v0.z, x[3] += v0.w;
-                        x[4] += v1.x, x[5] += v1.y, x[6] += v1.z, x[7] += v1.w;
+                    for (int n = 0; n < 8; ++n) {
+                        const float* x = o[m][8 * half + n] + 2 * i;
+                        *reinterpret_cast<float2*>(join + (wid * 8 + g) * 64 + ((8 * n + 2 * t) ^ (8 * (g & 3)))) =
+                            make_float2(x[0] * fix, x[1] * fix);
                     }
-                    if (whole) {
-                        const int node = (r0 + r) / P.group;
-                        const int64_t row = take.s.row0 + node, head = take.h * P.group + r0 + r - node * P.group;
-                        const float inv = lsum > 0.f ? 1.f / lsum : 0.f;
-                        uint4 v;
-                        v.x = Pair<T>::join(x[0] * inv, x[1] * inv);
-                        v.y = Pair<T>::join(x[2] * inv, x[3] * inv);
-                        v.z = Pair<T>::join(x[4] * inv, x[5] * inv);
-                        v.w = Pair<T>::join(x[6] * inv, x[7] * inv);
-                        *reinterpret_cast<uint4*>(static_cast<T*>(P.out.ptr) + row * P.out.token_stride + head * P.out.head_stride + 8 * c) = v;
-                        if (c == 0 && P.lse) P.lse[row * P.n_q_heads + head] = lsum > 0.f ? (high + log2f(lsum)) * 0x1.62e43p-1f : -INFINITY;
-                    } else {
-                        if (c == 0) {
-                            part[r0 + r] = high;
-                            part[L::kRows + r0 + r] = lsum;
+                    __syncthreads();
+                    if (r0 + r < rows) {
+                        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                        for (int w = 0; w < kWarps; ++w) {
+                            const float4 v = *reinterpret_cast<const float4*>(join + (w * 8 + r) * 64 + ((4 * c) ^ (8 * (r & 3))));
+                            x.x += v.x, x.y += v.y, x.z += v.z, x.w += v.w;
                         }
-                        float4* to = reinterpret_cast<float4*>(part + 2 * L::kRows + (size_t)(r0 + r) * D + 8 * c);
-                        to[0] = make_float4(x[0], x[1], x[2], x[3]);
-                        to[1] = make_float4(x[4], x[5], x[6], x[7]);
+                        const int at = 64 * half + 4 * c;
+                        if (whole) {
+                            const uint2 v = make_uint2(Pair<T>::join(x.x * inv, x.y * inv), Pair<T>::join(x.z * inv, x.w * inv));
+                            *reinterpret_cast<uint2*>(static_cast<T*>(P.out.ptr) + row * P.out.token_stride + head * P.out.head_stride + at) = v;
+                        } else {
+                            *reinterpret_cast<float4*>(part + 2 * L::kRows + (size_t)(r0 + r) * D + at) = x;
+                        }
+                    }
+                    __syncthreads();
+                }
+                if (c == 0 && r0 + r < rows) {
+                    if (!whole) {
+                        part[r0 + r] = high;
+                        part[L::kRows + r0 + r] = lsum;
+                    } else if (P.lse) {
+                        P.lse[row * P.n_q_heads + head] = lsum > 0.f ? (high + log2f(lsum)) * 0x1.62e43p-1f : -INFINITY;
                     }
                 }
-                __syncthreads();
             }
-        if (tid == 0 && part_begin == 0 && !whole) {  // the last item of the range: later blocks end it
-            const int64_t item_begin = begin + count - (take.end - part_begin);
+        if (tid == 0 && take.begin == 0 && !whole) {  // the last item of the range: later blocks end it
             SplitSlot d;
             d.b = take.b;
             d.h = take.h;
-            d.last = block_of(item_begin + take.units - 1, total, blocks);
-            d.reserved = 0;
+            d.row0 = 0;
+            d.last = take.last_block(range);
             split_slots(P)[blockIdx.x] = d;
         }
-        take.next(P, part_begin);
+        take.next(P, kUnit, L::kRows);
     }
 }
 
@@ -432,16 +415,17 @@ template <typename T, int D, int kTiles>
 cudaError_t launch(const AttentionParams& p, cudaStream_t stream)
 {
     CUtensorMap k, v;
-    cudaError_t err = make_cache_maps(p, kChunk, &k, &v);
+    cudaError_t err = make_cache_maps(p, 16, &k, &v);
     if (err != cudaSuccess) return err;
-    constexpr int bytes = Layout<D, kTiles>::kBytes;
+    using L = Layout<D, kTiles>;
+    constexpr int bytes = L::kBytes;
     auto kernel = stream_kernel<T, D, kTiles>;
     err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
     if (err != cudaSuccess) return err;
-    const int blocks = stream_blocks();
+    const int blocks = sm_count() * L::kBlocksPerSm;
     err = launch_dependent(kernel, dim3(blocks), dim3(kThreads), bytes, 1, stream, k, v, p);
     if (err != cudaSuccess) return err;
-    return launch_merge(p, blocks, 16 * kTiles, stream);
+    return launch_merge(p, blocks, L::kRows, stream);
 }
 
 template <typename T>
@@ -454,11 +438,13 @@ cudaError_t launch_typed(const AttentionParams& p, cudaStream_t stream)
 
 }  // namespace
 
-int stream_blocks()
+size_t stream_workspace(int rows, int d)
 {
-    int dev = 0, sms = 0;
-    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
-    return sms * kBlocksPerSm;
+    const bool two = rows > 16;
+    const int per_sm = d == 64 ? (two ? Layout<64, 2>::kBlocksPerSm : Layout<64, 1>::kBlocksPerSm)
+                               : (two ? Layout<128, 2>::kBlocksPerSm : Layout<128, 1>::kBlocksPerSm);
+    const int blocks = sm_count() * per_sm;
+    return slots_bytes(blocks) + (size_t)blocks * 2 * part_floats(two ? 32 : 16, d) * sizeof(float);
 }
 
 cudaError_t launch_stream(const AttentionParams& p, cudaStream_t stream)

@@ -1,0 +1,534 @@
+// attention_tiles.cu -- tree attention where more than 32 query rows share a
+// KV head (see tree_attention.cu): both products on the tensor cores' tcgen05
+// path, 128 rows to a tile.
+//
+// S = Q K^T comes into tensor memory from shared memory; a warpgroup takes a
+// tile's rows, one a thread, so that the softmax needs no exchange between
+// threads; its probabilities go back to tensor memory in the dtype, over the
+// scores, as the A operand of O += P V.  O stays in tensor memory and is
+// rescaled only when a row's maximum has grown by 2^8 (a power of two less in
+// the sums changes no rounding that matters, and few tiles do).  One warp loads
+// keys and values by TMA into a ring, one thread issues the products.
+//
+// Up to 128 rows: the cache's bytes are the bound; 64 tokens a tile, two blocks
+// an SM, so that one block's begin and end of an item hide behind the other.
+// More: the tensor cores are; a block takes 256 rows as two tiles whose
+// softmaxes and products alternate, over 128 tokens at a time, which also
+// reads the cache half as often.
+#include <type_traits>
+
+#include "attention_internal.cuh"
+
+namespace ctr {
+namespace {
+
+constexpr float kSlack = 8.f;  // growth of a row's maximum, in powers of two, that is let pass
+template <typename T> struct Lift;  // the largest probability is about 2^kLift (and at most 2^(kLift + kSlack))
+template <> struct Lift<__nv_bfloat16> { static constexpr float k = 0.f; };
+template <> struct Lift<__half> { static constexpr float k = 7.f; };
+
+template <int D, int kTiles>
+struct Layout {
+    static constexpr int kRows = 128 * kTiles;                 // of an item
+    static constexpr int kKeys = kTiles == 1 ? 64 : 128;       // of a unit
+    static constexpr int kThreads = 128 * kTiles + 64;         // softmax warpgroups, a loading warp, an issuing warp
+    static constexpr int kBlocksPerSm = kTiles == 1 ? 2 : 1;
+    static constexpr int kSlot = kKeys * D * 2;                // bytes of a ring slot: a unit's keys or its values
+    static constexpr int kQ = kRows * D * 2;
+    static constexpr int kSlots = kTiles == 1 ? 5 : (D == 128 ? 5 : 8);
+    static constexpr int kRing = kQ;
+    // full [kSlots], empty [kSlots]; scores and probabilities of either region [2] each; queries and outputs of a tile
+    // [2] each; one for the end
+    static constexpr int kBars = kRing + kSlots * kSlot;
+    static constexpr int kNBars = 2 * kSlots + 9;
+    static constexpr int kScratch = kBars + kNBars * 8;
+    static constexpr int kBad = kScratch + (kThreads / 32 + 2) * 8;  // two words of new tokens with values not finite
+    static constexpr int kTmem = kBad + 16;
+    static constexpr int kBytes = kTmem + 16;
+    static constexpr int kColumns = kTiles == 1 ? 256 : 512;   // of tensor memory: two regions of scores, then outputs
+    static constexpr int kO = 2 * kKeys;
+};
+
+// byte offset of 16-byte piece c (of D / 8) of row r in a tile of `rows` rows: halves of 64 dimensions, 128-byte
+// rows, pieces swizzled by the row
+__device__ __forceinline__ uint32_t piece(int rows, int r, int c)
+{
+    return (uint32_t)((c >> 3) * rows * 128 + r * 128 + (((c & 7) ^ (r & 7)) << 4));
+}
+
+// ---------------------------------------------------------------- tcgen05
+// A shared-memory operand with 128-byte swizzle: start, the stride between 64-element blocks of a row-contiguous
+// (MN-major) operand, the stride between groups of 8 rows (1,024 bytes).
+__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t block_stride)
+{
+    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(block_stride >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 |
+           2ull << 61;
+}
+// kind::f16 with fp32 accumulators, M = 128: types of A and B, whether B is MN-major, N
+template <typename T>
+__host__ __device__ constexpr uint32_t instruction(bool b_mn_major, int n)
+{
+    const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
+    return 1u << 4 | type << 7 | type << 10 | (b_mn_major ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24;
+}
+__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
+        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+__device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
+{
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        : "memory");
+}
+// arrives on the barrier once every product issued before is done
+__device__ __forceinline__ void mma_commit(uint32_t bar)
+{
+    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+__device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
+__device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+// 32 or 64 columns of this warp's 32 lanes; the wait stands in the same statement, so that nothing can read a
+// register before it
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[32], uint32_t addr)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%32];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+          "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(addr)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_load(uint32_t (&r)[64], uint32_t addr)
+{
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,"
+        "%16,%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31}, [%64];\n\t"
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%32,%33,%34,%35,%36,%37,%38,%39,%40,%41,%42,%43,%44,%45,%46,%47,"
+        "%48,%49,%50,%51,%52,%53,%54,%55,%56,%57,%58,%59,%60,%61,%62,%63}, [%65];\n\t"
+        "tcgen05.wait::ld.sync.aligned;"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+          "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+          "=r"(r[14]), "=r"(r[15]), "=r"(r[16]), "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]),
+          "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]), "=r"(r[25]), "=r"(r[26]), "=r"(r[27]),
+          "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31]), "=r"(r[32]), "=r"(r[33]), "=r"(r[34]),
+          "=r"(r[35]), "=r"(r[36]), "=r"(r[37]), "=r"(r[38]), "=r"(r[39]), "=r"(r[40]), "=r"(r[41]),
+          "=r"(r[42]), "=r"(r[43]), "=r"(r[44]), "=r"(r[45]), "=r"(r[46]), "=r"(r[47]), "=r"(r[48]),
+          "=r"(r[49]), "=r"(r[50]), "=r"(r[51]), "=r"(r[52]), "=r"(r[53]), "=r"(r[54]), "=r"(r[55]),
+          "=r"(r[56]), "=r"(r[57]), "=r"(r[58]), "=r"(r[59]), "=r"(r[60]), "=r"(r[61]), "=r"(r[62]),
+          "=r"(r[63])
+        : "r"(addr), "r"(addr + 32)
+        : "memory");
+}
+__device__ __forceinline__ void tmem_store(uint32_t addr, const uint32_t (&r)[32])
+{
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};" ::"r"(addr),
+        "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+        "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]),
+        "r"(r[21]), "r"(r[22]), "r"(r[23]), "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]),
+        "r"(r[31])
+        : "memory");
+}
+__device__ __forceinline__ void tmem_wait_store() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+template <typename T, int D, int kTiles>
+__global__ void __launch_bounds__(Layout<D, kTiles>::kThreads, (Layout<D, kTiles>::kBlocksPerSm))
+tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const AttentionParams P)
+{
+    using L = Layout<D, kTiles>;
+    constexpr int kKeys = L::kKeys, kSlots = L::kSlots;
+    extern __shared__ __align__(1024) unsigned char smem[];
+    const uint32_t base = smem_u32(smem), ring = base + L::kRing, full = base + L::kBars, empty = full + 8 * kSlots;
+    const uint32_t q_full = empty + 8 * kSlots, s_full = q_full + 16, p_full = s_full + 16, o_full = p_full + 16, done = o_full + 16;
+    const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
+    volatile uint32_t* tmem_at = reinterpret_cast<volatile uint32_t*>(smem + L::kTmem);
+    unsigned long long* bad_tokens = reinterpret_cast<unsigned long long*>(smem + L::kBad);
+
+    if (tid == 0) {
+        for (int i = 0; i < 2 * kSlots; ++i) bar_init(full + 8 * i, 1);
+        for (int i = 0; i < 2; ++i) {
+            bar_init(q_full + 8 * i, 128);
+            bar_init(s_full + 8 * i, 1);
+            bar_init(p_full + 8 * i, 128);
+            bar_init(o_full + 8 * i, 1);
+        }
+        bar_init(done, 1);
+        bad_tokens[0] = bad_tokens[1] = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
+    }
+    wait_for_previous_kernels();
+    const Range range = find_range<L::kThreads>(P, kKeys, L::kRows, blockIdx.x, gridDim.x, reinterpret_cast<int64_t*>(smem + L::kScratch));
+    if (tid == 0) split_slots(P)[blockIdx.x].b = -1;
+    if (range.end <= range.begin) return;  // the whole block, before it holds any tensor memory
+    if (wid == 0) {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::kTmem), "r"((uint32_t)L::kColumns)
+                     : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        fence_before();
+    }
+    __syncthreads();
+    fence_after();
+    const uint32_t tmem = *tmem_at;
+
+    bool fine = true;  // no wait of this warp (thread, where one thread acts) has run out: after one has, it only walks to the end
+    auto wait_thread = [&](uint32_t bar, uint32_t parity) {
+        if (fine && !bar_wait(bar, parity)) {
+            fine = false;
+            if (P.status) atomicExch(P.status, CTR_ETIMEOUT);
+        }
+        return fine;
+    };
+    auto wait_warp = [&](uint32_t bar, uint32_t parity) {
+        wait_thread(bar, parity);
+        return fine = __all_sync(~0u, fine);
+    };
+    // Scores and probabilities of unit u (of the block) of a tile: two tiles have a region each, one tile takes the two
+    // in turn, so that the next unit's scores need not wait for this one's softmax.
+    auto region_of = [](int tile, uint32_t u) { return kTiles == 1 ? (int)(u & 1) : tile; };
+    auto parity_of = [](uint32_t u) { return kTiles == 1 ? u >> 1 & 1 : u & 1; };
+    Walk w;
+    w.start(P, range, kKeys, L::kRows);
+
+    if (wid == 4 * kTiles) {
+        // ------------------------------------------------ loads: of each unit the keys, then the values
+        const int box = min(P.cache.page_tokens, kKeys), boxes = kKeys / box;
+        uint32_t n = 0, issued = 0;
+        for (; w.more(); w.next(P, kKeys, L::kRows)) {
+            const int head = w.h / (w.items / P.cache.n_kv_heads);
+            for (; w.u < w.end; ++w.u) {
+                const int key = w.u * kKeys + lane * box;
+                int page = -1;  // past the end: reads zeros
+                if (lane < boxes && key < w.s.len) page = __ldg(P.page_table + (int64_t)w.b * P.table_stride + (key >> P.page_log2));
+                for (int v = 0; v < 2; ++v, ++n) {
+                    const uint32_t slot = n % kSlots, at = ring + slot * L::kSlot + lane * box * 128;
+                    if (n >= kSlots) wait_warp(empty + 8 * slot, (n / kSlots + 1) & 1);
+                    if (!fine) continue;
+                    if (lane == 0) bar_expect(full + 8 * slot, L::kSlot);
+                    __syncwarp();
+                    if (lane < boxes) {
+                        const int y = key & (P.cache.page_tokens - 1);
+#pragma unroll
+                        for (int i = 0; i < D / 64; ++i)
+                            tma_load(at + i * kKeys * 128, v ? &map_v : &map_k, full + 8 * slot, 64 * i, y, head, page);
+                    }
+                    issued = n + 1;
+                }
+            }
+        }
+        // every load issued has landed before the block leaves (bounded again where a wait has run out)
+        for (uint32_t i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i) bar_wait(full + 8 * (i % kSlots), (i / kSlots) & 1);
+    } else if (wid == 4 * kTiles + 1) {
+        // ------------------------------------------------ products, issued by one thread
+        if (lane == 0) {
+            constexpr uint32_t kScores = instruction<T>(false, kKeys), kValues = instruction<T>(true, D);
+            uint32_t n = 0, items = 0, units = 0;  // ring slots used, items and units begun
+            auto scores = [&](int t, uint32_t slot, int region) {
+                const uint32_t q = base + t * 128 * D * 2, k = ring + slot * L::kSlot;
+#pragma unroll
+                for (int i = 0; i < D / 16; ++i)
+                    mma_shared(tmem + region * kKeys, operand(q + (i >> 2) * 128 * 128 + (i & 3) * 32, 16),
+                               operand(k + (i >> 2) * kKeys * 128 + (i & 3) * 32, 16), kScores, i > 0);
+                mma_commit(s_full + 8 * region);
+            };
+            auto values = [&](int t, uint32_t slot, int region, bool add) {
+                const uint32_t v = ring + slot * L::kSlot;
+#pragma unroll
+                for (int i = 0; i < kKeys / 16; ++i)
+                    mma_tensor(tmem + L::kO + t * D, tmem + region * kKeys + 8 * i, operand(v + i * 2048, kKeys * 128), kValues, add || i > 0);
+                mma_commit(o_full + 8 * t);
+            };
+            for (; w.more(); w.next(P, kKeys, L::kRows), ++items) {
+                const int count = w.end - w.begin;
+                for (int t = 0; t < kTiles; ++t) wait_thread(q_full + 8 * t, items & 1);
+                if (!wait_thread(full + 8 * (n % kSlots), (n / kSlots) & 1)) continue;
+                fence_after();
+                for (int t = 0; t < kTiles; ++t) scores(t, n % kSlots, region_of(t, units));
+                mma_commit(empty + 8 * (n % kSlots));
+                for (int i = 0; i < count && fine; ++i, n += 2, ++units) {
+                    // the next unit's scores go ahead of this one's values where they have a region of their own (one
+                    // tile), else right behind each tile's values: the softmax of one tile runs beside the other's products
+                    const uint32_t next = n + 2, value_slot = (n + 1) % kSlots;
+                    const bool more = i + 1 < count;
+                    auto wait_next = [&]() {
+                        const bool ok = wait_thread(full + 8 * (next % kSlots), (next / kSlots) & 1);
+                        fence_after();
+                        return ok;
+                    };
+                    if (kTiles == 1 && more) {
+                        if (!wait_next()) break;
+                        scores(0, next % kSlots, region_of(0, units + 1));
+                        mma_commit(empty + 8 * (next % kSlots));
+                    }
+                    for (int t = 0; t < kTiles; ++t) {
+                        if (!wait_thread(p_full + 8 * region_of(t, units), parity_of(units))) break;
+                        if (t == 0 && !wait_thread(full + 8 * value_slot, ((n + 1) / kSlots) & 1)) break;
+                        fence_after();
+                        values(t, value_slot, region_of(t, units), i > 0);
+                        if (t == kTiles - 1) mma_commit(empty + 8 * value_slot);
+                        if (kTiles > 1 && more) {
+                            if (t == 0 && !wait_next()) break;
+                            scores(t, next % kSlots, t);
+                            if (t == kTiles - 1) mma_commit(empty + 8 * (next % kSlots));
+                        }
+                    }
+                }
+            }
+            mma_commit(done);  // every product is done before the tensor memory is given back
+            bar_wait(done, 0);
+        }
+        __syncwarp();
+    } else {
+        // ------------------------------------------------ softmax: a row a thread
+        const int tile = wid >> 2, r = tid & 127;
+        const uint32_t lanes = (uint32_t)(32 * (wid & 3)) << 16;
+        const uint32_t o_at = tmem + lanes + L::kO + tile * D;
+        const float scale = P.scale_log2 == 0.f ? 1.f : fabsf(P.scale_log2);
+        uint32_t units = 0, items = 0;
+        for (; w.more(); w.next(P, kKeys, L::kRows), ++items) {
+            const int groups = w.items / P.cache.n_kv_heads, head = w.h / groups;
+            const int row = (w.h - head * groups) * L::kRows + tile * 128 + r;
+            const bool is = row < w.s.n_new * P.group;
+            const int node = is ? node_of(P, row) : 0;
+            const int64_t at = w.s.row0 + node, q_head = head * P.group + row - node * P.group;
+            const uint64_t mask = !is ? 0 : P.tree_mask ? __ldg(reinterpret_cast<const unsigned long long*>(P.tree_mask) + at) : ~0ull >> (63 - node);
+            // all rows begin an item together: no thread still reads the word of bad tokens that the next item takes
+            asm volatile("bar.sync 1, %0;" ::"r"(128 * kTiles) : "memory");
+            if (tid == 0) bad_tokens[(items + 1) & 1] = 0;
+            {
+                // The queries of this row; the last scores of the item before are done.  A negative scale turns them round,
+                // a scale of 0 is a query of zeros: the factor that the maxima and exponents take is positive.
+                const T* src = static_cast<const T*>(P.q.ptr) + at * P.q.token_stride + q_head * P.q.head_stride;
+                const uint32_t turn = P.scale_log2 < 0.f ? 0x80008000u : 0u;
+                uint4 v[D / 8];
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) v[c] = is ? __ldg(reinterpret_cast<const uint4*>(src) + c) : make_uint4(0, 0, 0, 0);
+#pragma unroll
+                for (int c = 0; c < D / 8; ++c) {
+                    v[c].x ^= turn, v[c].y ^= turn, v[c].z ^= turn, v[c].w ^= turn;
+                    if (P.scale_log2 == 0.f) v[c] = make_uint4(0, 0, 0, 0);
+                    *reinterpret_cast<uint4*>(smem + tile * 128 * D * 2 + piece(128, r, c)) = v[c];
+                }
+                fence_async();
+                bar_arrive(q_full + 8 * tile);
+            }
+            float top = -INFINITY, sum = 0.f;  // top: what the exponents are relative to, 2^-kLift of the largest
+            for (; w.u < w.end; ++w.u, ++units) {
+                const int key = w.u * kKeys;
+                const int region = region_of(tile, units);
+                const uint32_t s_at = tmem + lanes + region * kKeys;
+                float s[kKeys];
+                if (!wait_warp(s_full + 8 * region, parity_of(units))) continue;
+                fence_after();
+#pragma unroll
+                for (int c = 0; c < kKeys / 64; ++c) {
+                    uint32_t x[64];
+                    tmem_load(x, s_at + 64 * c);
+#pragma unroll
+                    for (int i = 0; i < 64; ++i) s[64 * c + i] = __uint_as_float(x[i]);
+                }
+                const bool edge = key + kKeys > w.s.context;
+                if (edge) {
+#pragma unroll
+                    for (int c = 0; c < kKeys / 32; ++c) {
+                        const uint32_t seen = is ? key + 32 * c < w.s.len ? seen_tokens(w.s, mask, key + 32 * c) : 0u : 0u;
+#pragma unroll
+                        for (int i = 0; i < 32; ++i)
+                            if (!(seen >> i & 1)) s[32 * c + i] = -INFINITY;
+                    }
+                }
+                float most[4] = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+#pragma unroll
+                for (int i = 0; i < kKeys; ++i) most[i & 3] = fmaxf(most[i & 3], s[i]);
+                const float high = fmaxf(fmaxf(most[0], most[1]), fmaxf(most[2], most[3])) * scale - Lift<T>::k;
+                const bool first = w.u == w.begin;
+                const bool grown = first ? high > top : high > top + kSlack || (top == -INFINITY && high > top);
+                if (__any_sync(~0u, grown)) {
+                    const float fix = grown ? exp2_fast(top - high) : 1.f;
+                    if (grown) {
+                        top = high;
+                        sum *= fix;
+                    }
+                    if (!first && wait_warp(o_full + 8 * tile, (units - 1) & 1)) {  // the values of the unit before
+                        fence_after();
+#pragma unroll
+                        for (int c = 0; c < D / 32; ++c) {
+                            uint32_t x[32];
+                            tmem_load(x, o_at + 32 * c);
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) x[i] = __float_as_uint(__uint_as_float(x[i]) * fix);
+                            tmem_store(o_at + 32 * c, x);
+                        }
+                    }
+                }
+                const float ref = top == -INFINITY ? 0.f : top;
+                float part[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int c = 0; c < kKeys / 64; ++c) {
+                    uint32_t x[32];
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const float a = exp2_fast(fmaf(s[64 * c + 2 * i], scale, -ref)), b = exp2_fast(fmaf(s[64 * c + 2 * i + 1], scale, -ref));
+                        part[(2 * i) & 3] += a;
+                        part[(2 * i + 1) & 3] += b;
+                        x[i] = Pair<T>::join(a, b);
+                    }
+                    tmem_store(s_at + 32 * c, x);
+                }
+                sum += (part[0] + part[1]) + (part[2] + part[3]);
+                if (edge && tile == 0) {
+                    // Values that no row may see, or only some: those past the end become zeros, and a new token's that are
+                    // not finite too, to be added at the end to the rows that attend to it.
+                    const uint32_t n = 2 * units + 1, slot = n % kSlots;
+                    if (wait_warp(full + 8 * slot, (n / kSlots) & 1) && r < kKeys) {
+                        unsigned char* values = smem + L::kRing + slot * L::kSlot;
+                        const int p = key + r, new_token = p - w.s.context;
+                        if (p >= w.s.len) {
+#pragma unroll
+                            for (int c = 0; c < D / 8; ++c) *reinterpret_cast<uint4*>(values + piece(kKeys, r, c)) = make_uint4(0, 0, 0, 0);
+                        } else if (new_token >= 0) {
+                            uint32_t bad = 0;
+#pragma unroll
+                            for (int c = 0; c < D / 8; ++c) {
+                                const uint4 v = *reinterpret_cast<const uint4*>(values + piece(kKeys, r, c));
+                                bad |= not_finite<T>(v.x) | not_finite<T>(v.y) | not_finite<T>(v.z) | not_finite<T>(v.w);
+                            }
+                            if (__builtin_expect(bad != 0, 0)) {
+                                for (int c = 0; c < D / 2; ++c) {
+                                    uint32_t* v = reinterpret_cast<uint32_t*>(values + piece(kKeys, r, c >> 2)) + (c & 3);
+                                    const uint32_t b = not_finite<T>(*v);
+                                    *v &= ~((b & 0x8000u ? 0xffffu : 0u) | (b & 0x80000000u ? 0xffff0000u : 0u));
+                                }
+                                atomicOr(bad_tokens + (items & 1), 1ull << (new_token & 63));
+                            }
+                        }
+                    }
+                    fence_async();
+                }
+                // no tile gets two products with its values ahead: a parity tells the last one's end from the one before
+                if (!first) wait_warp(o_full + 8 * tile, (units - 1) & 1);
+                tmem_wait_store();
+                fence_before();
+                bar_arrive(p_full + 8 * region);
+            }
+            // the sums of this part of the item
+            wait_warp(o_full + 8 * tile, (units - 1) & 1);
+            fence_after();
+            const bool whole = w.begin == 0 && w.end == w.units;
+            const float inv = whole ? (sum > 0.f ? 1.f / sum : 0.f) : 1.f;
+            const uint64_t bad = is && fine ? bad_tokens[items & 1] & mask : 0;
+            float* part = part_of_item(P, gridDim.x, L::kRows, D, blockIdx.x, w.begin == 0 ? 1 : 0);
+            const int part_row = tile * 128 + r;
+#pragma unroll
+            for (int c = 0; c < D / 32; ++c) {
+                uint32_t x[32];
+                tmem_load(x, o_at + 32 * c);
+                for (uint64_t todo = bad; __builtin_expect(todo != 0, 0); todo &= todo - 1) {  // from the cache
+                    const int p = w.s.context + __ffsll(todo) - 1;
+                    const int64_t page = P.page_table[(int64_t)w.b * P.table_stride + (p >> P.page_log2)];
+                    const T* v = static_cast<const T*>(P.cache.v) + page * P.cache.page_stride + head * P.cache.head_stride +
+                                 (p & (P.cache.page_tokens - 1)) * P.cache.token_stride + 32 * c;
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const float f = to_float(v[i]);
+                        if (!(fabsf(f) < INFINITY)) x[i] = __float_as_uint(__uint_as_float(x[i]) + f);
+                    }
+                }
+                if (is && fine) {
+                    if (whole) {
+                        uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(P.out.ptr) + at * P.out.token_stride + q_head * P.out.head_stride + 32 * c);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t v[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j)
+                                v[j] = Pair<T>::join(__uint_as_float(x[8 * i + 2 * j]) * inv, __uint_as_float(x[8 * i + 2 * j + 1]) * inv);
+                            to[i] = make_uint4(v[0], v[1], v[2], v[3]);
+                        }
+                    } else {
+                        uint4* to = reinterpret_cast<uint4*>(part + 2 * L::kRows + (size_t)part_row * D + 32 * c);
+#pragma unroll
+                        for (int i = 0; i < 8; ++i) to[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                    }
+                }
+                __syncwarp();
+            }
+            if (is && fine) {
+                if (!whole) {
+                    part[part_row] = top;
+                    part[L::kRows + part_row] = sum;
+                } else if (P.lse) {
+                    P.lse[at * P.n_q_heads + q_head] = sum > 0.f ? (top + log2f(sum)) * 0x1.62e43p-1f : -INFINITY;
+                }
+            }
+            if (tid == 0 && w.begin == 0 && !whole) {  // the last item of the range: later blocks end it
+                SplitSlot d;
+                d.b = w.b;
+                d.h = head;
+                d.row0 = row;
+                d.last = w.last_block(range);
+                split_slots(P)[blockIdx.x] = d;
+            }
+            fence_before();
+        }
+    }
+    __syncthreads();
+    if (wid == 0) {
+        fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"((uint32_t)L::kColumns) : "memory");
+    }
+}
+
+template <typename T, int D, int kTiles>
+cudaError_t launch(const AttentionParams& p, cudaStream_t stream)
+{
+    using L = Layout<D, kTiles>;
+    CUtensorMap k, v;
+    cudaError_t err = make_cache_maps(p, p.cache.page_tokens < L::kKeys ? p.cache.page_tokens : L::kKeys, &k, &v);
+    if (err != cudaSuccess) return err;
+    auto kernel = tiles_kernel<T, D, kTiles>;
+    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+    if (err != cudaSuccess) return err;
+    const int blocks = sm_count() * L::kBlocksPerSm;
+    err = launch_dependent(kernel, dim3(blocks), dim3(L::kThreads), L::kBytes, 1, stream, k, v, p);
+    if (err != cudaSuccess) return err;
+    return launch_merge(p, blocks, L::kRows, stream);
+}
+
+template <typename T>
+cudaError_t launch_typed(const AttentionParams& p, cudaStream_t stream)
+{
+    const bool two = p.group * p.max_nodes > 128;
+    if (p.cache.head_dim == 64) return two ? launch<T, 64, 2>(p, stream) : launch<T, 64, 1>(p, stream);
+    return two ? launch<T, 128, 2>(p, stream) : launch<T, 128, 1>(p, stream);
+}
+
+}  // namespace
+
+size_t tiles_workspace(int rows, int d)
+{
+    const int tiles = rows > 128 ? 2 : 1, blocks = sm_count() * (tiles == 1 ? 2 : 1);
+    return slots_bytes(blocks) + (size_t)blocks * 2 * part_floats(128 * tiles, d) * sizeof(float);
+}
+
+cudaError_t launch_tiles(const AttentionParams& p, cudaStream_t stream)
+{
+    return p.cache.dtype == CTR_BF16 ? launch_typed<__nv_bfloat16>(p, stream) : launch_typed<__half>(p, stream);
+}
+
+}  // namespace ctr

@@ -132,6 +132,7 @@ int ctr_tree_attention(const ctr_kv_cache* cache, ctr_rows q, ctr_rows out, int6
     p.page_table = page_table;
     p.tree_mask = tree_mask;
     p.scale_log2 = (float)((double)scale * 1.4426950408889634);
+    p.group_magic = ((1u << 20) + (uint32_t)p.group - 1) / (uint32_t)p.group;
     p.lse = lse;
     p.status = status;
     p.ws = static_cast<unsigned char*>(workspace);

@@ -51,9 +51,10 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
-// two values in one 32-bit register, the first in the low half
+// two values in one 32-bit register, the first in the low half; kExpOne: the unit of both exponents
 template <typename T> struct Pair;
 template <> struct Pair<__nv_bfloat16> {
+    static constexpr uint32_t kExpOne = 0x00800080u;
     static __device__ __forceinline__ float2 split(uint32_t v)
     {
         return make_float2(__uint_as_float(v << 16), __uint_as_float(v & 0xffff0000u));
@@ -66,6 +67,7 @@ template <> struct Pair<__nv_bfloat16> {
     }
 };
 template <> struct Pair<__half> {
+    static constexpr uint32_t kExpOne = 0x04000400u;
     static __device__ __forceinline__ float2 split(uint32_t v)
     {
         __half2 h;
@@ -79,6 +81,13 @@ template <> struct Pair<__half> {
         return r;
     }
 };
+
+// sign bits set where a half is infinite or NaN: an exponent of all ones carries into it
+template <typename T>
+__device__ __forceinline__ uint32_t not_finite(uint32_t v)
+{
+    return ((v & 0x7fff7fffu) + Pair<T>::kExpOne) & 0x80008000u;
+}
 
 // ---------------------------------------------------------------- cache append
 struct AppendParams {
@@ -104,6 +113,7 @@ struct AttentionParams {
     const int32_t* page_table;
     const uint64_t* tree_mask;
     float scale_log2;           // scale times log2 e
+    uint32_t group_magic;       // ceil(2^20 / group): r / group = r * magic >> 20 for the rows r < 64 group
     float* lse;
     int32_t* status;
     unsigned char* ws;

@@ -14,133 +14,93 @@ namespace {
 
 constexpr int kThreads = 128;
 
+// The items that several blocks worked on, a row at a time: its parts in the order of the blocks.  Where a row has few
+// parts each warp takes a row (kSplit = 1), else the block's warps take a fourth of one row's parts each.
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) attention_kernel(const AttentionParams P)
-{
-    constexpr int kPer = D / 32;  // dimensions of a lane
-    __shared__ float sm_o[kThreads / 32][D], sm_m[kThreads / 32], sm_l[kThreads / 32];
-    wait_for_previous_kernels();
-    const int b = blockIdx.x / P.max_nodes, node = blockIdx.x % P.max_nodes, h = blockIdx.y;
-    const Seq s = seq_of(P, b);
-    if (node >= s.n_new) return;
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5;
-    const int64_t row = s.row0 + node;
-    const uint64_t mask = P.tree_mask ? P.tree_mask[row] : ~0ull >> (63 - node);
-    const int64_t head = (h / P.group) * P.cache.head_stride;
-    const T* q = static_cast<const T*>(P.q.ptr) + row * P.q.token_stride + h * P.q.head_stride + lane * kPer;
-    float qv[kPer], o[kPer], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-        qv[j] = to_float(q[j]);
-        o[j] = 0.f;
-    }
-    for (int p = wid; p < s.len; p += kThreads / 32) {
-        const int n = p - s.context;
-        if (n >= 0 && !(mask >> n & 1)) continue;
-        const int64_t page = P.page_table[(int64_t)b * P.table_stride + (p >> P.page_log2)];
-        const bool there = page >= 0 && page < P.cache.n_pages;
-        const int64_t at = page * P.cache.page_stride + head + (p & (P.cache.page_tokens - 1)) * P.cache.token_stride + lane * kPer;
-        float dot = 0.f, v[kPer];
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) {
-            dot += qv[j] * (there ? to_float(static_cast<const T*>(P.cache.k)[at + j]) : 0.f);
-            v[j] = there ? to_float(static_cast<const T*>(P.cache.v)[at + j]) : 0.f;
-        }
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) dot += __shfl_xor_sync(~0u, dot, off);
-        dot *= P.scale_log2;
-        const float mn = fmaxf(m, dot), fix = m == -INFINITY ? 0.f : exp2f(m - mn), w = exp2f(dot - mn);
-        l = l * fix + w;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) o[j] = o[j] * fix + w * v[j];
-        m = mn;
-    }
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) sm_o[wid][lane * kPer + j] = o[j];
-    sm_m[wid] = m;
-    sm_l[wid] = l;
-    __syncthreads();
-    float top = -INFINITY;
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) top = fmaxf(top, sm_m[w]);
-    float sum = 0.f, part[kThreads / 32];
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-        part[w] = sm_m[w] == -INFINITY ? 0.f : exp2f(sm_m[w] - top);
-        sum += part[w] * sm_l[w];
-    }
-    T* out = static_cast<T*>(P.out.ptr) + row * P.out.token_stride + h * P.out.head_stride;
-    for (int j = threadIdx.x; j < D; j += kThreads) {
-        float acc = 0.f;
-#pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) acc += part[w] * sm_o[w][j];
-        out[j] = from_float<T>(sum > 0.f ? acc / sum : 0.f);
-    }
-    if (threadIdx.x == 0 && P.lse)
-        P.lse[row * P.n_q_heads + h] = sum > 0.f ? (top + log2f(sum)) * 0x1.62e43p-1f : -INFINITY;
-}
+struct MergedRow {
+    static constexpr int kPer = D / 32;
+    float o[kPer], m, l;
 
-// One row of an item that several blocks worked on: their parts in the order of the blocks, a fourth of them to a warp.
-template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P, int blocks, int rows)
-{
-    constexpr int kPer = D / 32;
-    __shared__ float sm_o[kThreads / 32][D], sm_m[kThreads / 32], sm_l[kThreads / 32];
-    wait_for_previous_kernels();
-    const SplitSlot d = split_slots(P)[blockIdx.x];
-    if (d.b < 0) return;
-    const Seq s = seq_of(P, d.b);
-    const int r = blockIdx.y;
-    if (r >= s.n_new * P.group) return;
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, first = blockIdx.x, n = d.last - first + 1;
-    float o[kPer], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int j = 0; j < kPer; ++j) o[j] = 0.f;
-    const int per = (n + kThreads / 32 - 1) / (kThreads / 32);
-#pragma unroll 4
-    for (int i = wid * per; i < min((wid + 1) * per, n); ++i) {
-        const float* part = part_of_item(P, blocks, rows, D, first + i, i == 0 ? 1 : 0);
-        const float pm = part[r], pl = part[rows + r];
-        float po[kPer];
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) po[j] = part[2 * rows + (size_t)r * D + lane * kPer + j];
+    __device__ __forceinline__ void add(float pm, float pl, const float (&po)[kPer])
+    {
         const float mn = fmaxf(m, pm), fa = m == -INFINITY ? 0.f : exp2_fast(m - mn), fb = pm == -INFINITY ? 0.f : exp2_fast(pm - mn);
         l = l * fa + pl * fb;
 #pragma unroll
         for (int j = 0; j < kPer; ++j) o[j] = o[j] * fa + (pm == -INFINITY ? 0.f : po[j] * fb);
         m = mn;
     }
+    // parts [from, to) of row r of the item that block `first` begins
+    __device__ __forceinline__ void gather(const AttentionParams& P, int blocks, int rows, int r, int first, int from, int to, int lane)
+    {
+        m = -INFINITY;
+        l = 0.f;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) sm_o[wid][lane * kPer + j] = o[j];
-    sm_m[wid] = m;
-    sm_l[wid] = l;
-    __syncthreads();
-    float top = -INFINITY, sum = 0.f, part[kThreads / 32];
+        for (int j = 0; j < kPer; ++j) o[j] = 0.f;
+#pragma unroll 4
+        for (int i = from; i < to; ++i) {
+            const float* part = part_of_item(P, blocks, rows, D, first + i, i == 0 ? 1 : 0);
+            float po[kPer];
 #pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) top = fmaxf(top, sm_m[w]);
-#pragma unroll
-    for (int w = 0; w < kThreads / 32; ++w) {
-        part[w] = sm_m[w] == -INFINITY ? 0.f : exp2_fast(sm_m[w] - top);
-        sum += part[w] * sm_l[w];
+            for (int j = 0; j < kPer; ++j) po[j] = part[2 * rows + (size_t)r * D + lane * kPer + j];
+            add(part[r], part[rows + r], po);
+        }
     }
-    const int node = r / P.group;
-    const int64_t row = s.row0 + node, h = d.h * P.group + r - node * P.group;
-    T* out = static_cast<T*>(P.out.ptr) + row * P.out.token_stride + h * P.out.head_stride;
-    for (int j = threadIdx.x; j < D; j += kThreads) {
-        float acc = 0.f;
+    __device__ __forceinline__ void write(const AttentionParams& P, const Seq& s, const SplitSlot& d, int r, int lane) const
+    {
+        const int node = node_of(P, d.row0 + r);
+        const int64_t row = s.row0 + node, h = d.h * P.group + d.row0 + r - node * P.group;
+        T* out = static_cast<T*>(P.out.ptr) + row * P.out.token_stride + h * P.out.head_stride + lane * kPer;
+        const float inv = l > 0.f ? 1.f / l : 0.f;
+        uint32_t v[kPer / 2];
 #pragma unroll
-        for (int w = 0; w < kThreads / 32; ++w) acc += part[w] == 0.f ? 0.f : part[w] * sm_o[w][j];
-        out[j] = from_float<T>(sum > 0.f ? acc / sum : 0.f);
+        for (int j = 0; j < kPer / 2; ++j) v[j] = Pair<T>::join(o[2 * j] * inv, o[2 * j + 1] * inv);
+#pragma unroll
+        for (int j = 0; j < kPer / 2; ++j) reinterpret_cast<uint32_t*>(out)[j] = v[j];
+        if (lane == 0 && P.lse) P.lse[row * P.n_q_heads + h] = l > 0.f ? (m + log2f(l)) * 0x1.62e43p-1f : -INFINITY;
     }
-    if (threadIdx.x == 0 && P.lse) P.lse[row * P.n_q_heads + h] = sum > 0.f ? (top + log2f(sum)) * 0x1.62e43p-1f : -INFINITY;
-}
+};
 
-template <typename T>
-cudaError_t launch_typed(const AttentionParams& p, cudaStream_t stream)
+constexpr int kFewParts = 8;
+
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P, int blocks, int rows)
 {
-    const dim3 grid((unsigned)(p.n_seqs * p.max_nodes), (unsigned)p.n_q_heads);
-    if (p.cache.head_dim == 64) return launch_dependent(attention_kernel<T, 64>, grid, dim3(kThreads), 0, 1, stream, p);
-    return launch_dependent(attention_kernel<T, 128>, grid, dim3(kThreads), 0, 1, stream, p);
+    constexpr int kPer = D / 32, kWarps = kThreads / 32;
+    __shared__ float sm_o[kWarps][D], sm_m[kWarps], sm_l[kWarps];
+    wait_for_previous_kernels();
+    const SplitSlot d = split_slots(P)[blockIdx.x];
+    if (d.b < 0) return;
+    const Seq s = seq_of(P, d.b);
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, first = blockIdx.x, n = d.last - first + 1;
+    const int end = min(rows, s.n_new * P.group - d.row0);
+    MergedRow<T, D> a;
+    if (n <= kFewParts) {
+        for (int r = blockIdx.y * kWarps + wid; r < end; r += gridDim.y * kWarps) {
+            a.gather(P, blocks, rows, r, first, 0, n, lane);
+            a.write(P, s, d, r, lane);
+        }
+        return;
+    }
+    const int per = (n + kWarps - 1) / kWarps;
+    for (int r = blockIdx.y; r < end; r += gridDim.y) {
+        a.gather(P, blocks, rows, r, first, min(wid * per, n), min((wid + 1) * per, n), lane);
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) sm_o[wid][lane * kPer + j] = a.o[j];
+        sm_m[wid] = a.m;
+        sm_l[wid] = a.l;
+        __syncthreads();
+        if (wid == 0) {
+#pragma unroll
+            for (int w = 1; w < kWarps; ++w) {
+                float po[kPer];
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) po[j] = sm_o[w][lane * kPer + j];
+                a.add(sm_m[w], sm_l[w], po);
+            }
+            a.write(P, s, d, r, lane);
+        }
+        __syncthreads();
+    }
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -165,6 +125,13 @@ constexpr int kStreamRows = 32;  // most rows of a KV head that the streaming ke
 
 }  // namespace
 
+int sm_count()
+{
+    int dev = 0, sms = 0;
+    if (cudaGetDevice(&dev) != cudaSuccess || cudaDeviceGetAttribute(&sms, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 0;
+    return sms;
+}
+
 // The cache as a 4-d tensor (dimension, token of a page, head, page) of boxes of 64 dimensions x box_tokens tokens;
 // a page outside it reads as zeros.
 cudaError_t make_cache_maps(const AttentionParams& p, int box_tokens, CUtensorMap* k, CUtensorMap* v)
@@ -185,7 +152,8 @@ cudaError_t make_cache_maps(const AttentionParams& p, int box_tokens, CUtensorMa
 
 cudaError_t launch_merge(const AttentionParams& p, int blocks, int rows, cudaStream_t stream)
 {
-    const dim3 grid((unsigned)blocks, (unsigned)(p.group * p.max_nodes));
+    const int most = p.group * p.max_nodes < rows ? p.group * p.max_nodes : rows;
+    const dim3 grid((unsigned)blocks, (unsigned)(most < 32 ? most : 32));
     const bool bf = p.cache.dtype == CTR_BF16, wide = p.cache.head_dim == 128;
     auto kernel = bf ? (wide ? merge_kernel<__nv_bfloat16, 128> : merge_kernel<__nv_bfloat16, 64>)
                      : (wide ? merge_kernel<__half, 128> : merge_kernel<__half, 64>);
@@ -195,15 +163,12 @@ cudaError_t launch_merge(const AttentionParams& p, int blocks, int rows, cudaStr
 size_t attention_workspace(const ctr_kv_cache& cache, int32_t n_q_heads, int32_t, int32_t max_nodes)
 {
     const int rows = n_q_heads / cache.n_kv_heads * max_nodes;
-    if (rows > kStreamRows) return 256;
-    const int blocks = stream_blocks();
-    return slots_bytes(blocks) + (size_t)blocks * 2 * part_floats(rows > 16 ? 32 : 16, cache.head_dim) * sizeof(float);
+    return rows > kStreamRows ? tiles_workspace(rows, cache.head_dim) : stream_workspace(rows, cache.head_dim);
 }
 
 cudaError_t launch_attention(const AttentionParams& p, cudaStream_t stream)
 {
-    if (p.group * p.max_nodes <= kStreamRows) return launch_stream(p, stream);
-    return p.cache.dtype == CTR_BF16 ? launch_typed<__nv_bfloat16>(p, stream) : launch_typed<__half>(p, stream);
+    return p.group * p.max_nodes <= kStreamRows ? launch_stream(p, stream) : launch_tiles(p, stream);
 }
 
 }  // namespace ctr
