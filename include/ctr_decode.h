@@ -137,7 +137,8 @@ int ctr_tree_attention(const ctr_kv_cache* cache /* host */, ctr_rows q, ctr_row
  * and the token is the first, in vocabulary order, at which the kept weights'
  * running sum exceeds floor(W' floor(2^31 u) / 2^31), W' their sum.
  * temperature[r] not > 0: the first in the order, whatever the rest says.
- * token[r] = -1, logprob[r] = -inf, n_kept[r] = 0 where no logit is above -inf.
+ * token[r] = -1, logprob[r] = -inf, n_kept[r] = 0 where no logit is above -inf
+ * (-1 and a NaN where a bounded wait of the kernel ran out, never expected).
  * logprob[r] = ln(w / W') of the token and n_kept[r] the number kept are
  * optional outputs; top_k, top_p and min_p optional inputs (NULL: off; a NaN
  * is off).  0 <= n_rows < 2^31, 1 <= vocab <= CTR_MAX_VOCAB, row_stride >= vocab. */
