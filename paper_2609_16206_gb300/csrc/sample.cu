@@ -9,16 +9,17 @@
 // copies; everything after is passes over that copy and exchanges of a few
 // words over the cluster.  The kept tokens are the ones before a cut in the
 // order (falling logits, then index):
-//   * few of them (top-k up to kList, or a nucleus that is): the k-th largest
-//     of the threads' own maxima is a bound that at least k logits reach and
-//     not many more do; those go to the first block's list, which ranks them;
+//   * few of them (top-k up to kList, or a nucleus that is): each warp's r-th
+//     largest of its lanes' maxima, the smallest of them over the cluster, is a
+//     bound that r logits of every warp reach and few others do; those go to
+//     the first block, which ranks them;
 //   * a nucleus cut off by min-p anyway needs no cut: the mass of what min-p
 //     keeps, summed with the whole row's, shows it;
-//   * else the cut is found from the mass (or count) in 512 bins of y, then in
-//     512 parts of the bin that holds it, then by bisection over the part's
+//   * else the cut is found from the masses (or counts) of 512 bins of y, then
+//     of 512 parts of the bin that holds it, then by bisection over the part's
 //     keys, and over equal keys by index.
-// The drawn token's block is known from the blocks' sums and finds it in a
-// pass of its own.
+// Warps take contiguous runs of a block's part, so that the warps' sums say
+// where the drawn token lies, and only that run is gone through again.
 #include "decode_internal.cuh"
 
 namespace ctr {
@@ -26,9 +27,8 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
-constexpr int kList = 128;          // tokens that the first block ranks
-constexpr int kMine = 512;          // candidates of a block
-constexpr int kGather = 1536;       // of the cluster
+constexpr int kList = 256;          // tokens that the first block ranks
+constexpr int kGather = 1536;       // candidates of the cluster, an equal share of them to a block
 constexpr int kBins = 512;
 constexpr int kPieces = 4;          // of a block's part of the row, each a bulk copy
 constexpr uint32_t kEmptyKey = 0;   // of -inf and NaN
@@ -119,19 +119,13 @@ __device__ __forceinline__ uint32_t part_of(float x, uint32_t most)
 }
 
 // ---------------------------------------------------------------- blocks and clusters
-struct Tally {
-    uint64_t a, b;
-    uint32_t n, top;
+struct Sums {  // of weights and a count
+    uint64_t a, b, c;
+    uint32_t n;
 };
-__device__ __forceinline__ Tally join(const Tally& x, const Tally& y)
-{
-    return Tally{x.a + y.a, x.b + y.b, x.n + y.n, x.top > y.top ? x.top : y.top};
-}
-__device__ __forceinline__ Tally shuffled(const Tally& v, int off)
-{
-    return Tally{__shfl_xor_sync(~0u, v.a, off), __shfl_xor_sync(~0u, v.b, off), __shfl_xor_sync(~0u, v.n, off),
-                 __shfl_xor_sync(~0u, v.top, off)};
-}
+struct Words {  // two maxima and a count
+    uint32_t top, high, n;
+};
 
 __device__ __forceinline__ uint32_t smem_u32(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
 __device__ __forceinline__ uint32_t cluster_rank()
@@ -160,6 +154,10 @@ __device__ __forceinline__ void remote_store(uint32_t addr, uint64_t v)
 {
     asm volatile("st.shared::cluster.u64 [%0], %1;" ::"r"(addr), "l"(v) : "memory");
 }
+__device__ __forceinline__ void remote_store32(uint32_t addr, uint32_t v)
+{
+    asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
+}
 __device__ __forceinline__ uint32_t remote_load(uint32_t addr)
 {
     uint32_t v;
@@ -168,15 +166,47 @@ __device__ __forceinline__ uint32_t remote_load(uint32_t addr)
 }
 struct __align__(16) Shared {
     uint64_t gather[kGather];       // first block: (key, ~index) of the candidates
-    uint64_t mine[kMine];           // this block's; later the ranked ones' weights
-    uint32_t bins[3][kBins];        // low and high halves of the masses, counts
-    Tally warp[kWarps];
-    Tally peers[2][kMaxCluster];    // exchanges alternate between the two
-    uint64_t prefix[kWarps];
-    uint64_t found[4];
-    uint32_t n_mine;
+    uint64_t list[kGather];         // the same without gaps, then the ranked ones'
+    uint32_t bins[3][kBins];        // low and high halves of the masses, counts; the ranked ones' weights
+    Sums warp[kWarps];
+    Words warp_words[kWarps];
+    Sums peers[2][kMaxCluster];     // exchanges alternate between the two
+    Words peer_words[2][kMaxCluster];
+    uint64_t warp_mass[kWarps];     // what each warp's run holds of the kept tokens
+    uint64_t found[3];
+    uint32_t counts[kMaxCluster];   // candidates of each block
+    uint32_t n_mine, n_list;
     uint64_t bar[kPieces];
 };
+
+// ln(w / mass) for 0 < w <= mass < 2^49, to about half a unit of fp32: the quotient as the sum q + r of two fp32, q =
+// 2^e m with m in [0.7, 1.42), ln m = 2 atanh((m - 1) / (m + 1)) by its series, whose first term is carried in two.
+__device__ __forceinline__ float log_share(uint32_t w, uint64_t mass)
+{
+    const float wh = __uint2float_rn(w), wl = (float)(int32_t)(w - (uint32_t)(uint64_t)wh);
+    const float mh = __ull2float_rn(mass), ml = (float)(int64_t)(mass - (uint64_t)mh);
+    const float q = wh / mh, r = (fmaf(-q, mh, wh) + (wl - q * ml)) / mh;
+    if (w == mass) return 0.f;
+    const uint32_t bits = __float_as_uint(q);
+    int e = (int)(bits >> 23) - 127;
+    float m = __uint_as_float((bits & 0x7fffffu) | 0x3f800000u);
+    if (m > 1.41421354f) {
+        m *= 0.5f;
+        e += 1;
+    }
+    const float n = m - 1.f, d = m + 1.f, dl = n - (d - 2.f);  // m + 1 = d + dl
+    const float s1 = n / d, s2 = (fmaf(-s1, d, n) - s1 * dl) / d, z = s1 * s1;
+    float p = 2.f / 13.f;
+    p = fmaf(p, z, 2.f / 11.f);
+    p = fmaf(p, z, 2.f / 9.f);
+    p = fmaf(p, z, 2.f / 7.f);
+    p = fmaf(p, z, 2.f / 5.f);
+    p = fmaf(p, z, 2.f / 3.f);
+    const float small = fmaf(p * z, s1, 2.f * s2) + r / q;
+    const float a = (float)e * 0x1.62e4p-1f, b = 2.f * s1;  // ln 2 in 16 bits and the rest: e times the first is exact
+    const float sum = a + b, t = sum - a, err = (a - (sum - t)) + (b - t);
+    return sum + (err + fmaf((float)e, 0x1.7f7d1cp-20f, small));
+}
 
 template <typename T> struct Vec {  // logits of 16 bytes
     static constexpr int kN = 8;
@@ -215,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     if (tid == 0) {
         for (int i = 0; i < kPieces; ++i) asm volatile("mbarrier.init.shared::cta.b64 [%0], 1;" ::"r"(smem_u32(&sm.bar[i])) : "memory");
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
-        sm.n_mine = 0;
+        sm.n_mine = sm.n_list = 0;
     }
     wait_for_previous_kernels();
 
@@ -227,7 +257,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const int base = v0 * kN - shift;                       // index of the part's first element
     const int whole0 = v0 == 0 && shift > 0 ? 1 : 0;        // vectors that lie inside the row
     const int whole1 = v0 + count == n_vec && (P.vocab + shift) % kN != 0 ? count - 1 : count;
-    const int piece = ((per + kPieces - 1) / kPieces + kThreads - 1) / kThreads * kThreads;
+    const int chunk = (per + kWarps - 1) / kWarps;          // vectors of a warp's run
+    const int piece = chunk * (kWarps / kPieces);
     __syncthreads();
     if (tid == 0) {
         for (int i = 0; i < kPieces; ++i) {
@@ -255,7 +286,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     const uint32_t u_part = part_of(P.u[row], 0x7fffffffu);
     __syncthreads();
 
-    // ---- the row's maximum, and this thread's
+    // ---- the row's maximum, this thread's, and the r-th largest of its warp's
     auto wait_piece = [&](int i) {
         uint32_t done = 0;
         for (unsigned it = 0; it < kWaitLimit && !done; ++it)
@@ -265,72 +296,128 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
                          : "memory");
         return done != 0;
     };
+    const int run0 = wid * chunk, run1 = min(run0 + chunk, count);  // this warp's run
     float most = -INFINITY;
-    bool fine = true;
-    for (int i = 0; i < kPieces; ++i) {
-        fine = wait_piece(i) && fine;
-        for (int v = i * piece + tid; v < min((i + 1) * piece, count); v += kThreads) {
-            float e[kN];
-            Vec<T>::split(part[v], e);
+    // (a block leaves only after every piece has landed: each has warps that wait for it, and the exchange is behind
+    // them; a wait that runs out, never expected, is given a second bound for that and spoils the row)
+    const bool fine = wait_piece(wid / (kWarps / kPieces));
+    if (!fine) wait_piece(wid / (kWarps / kPieces));
+    for (int v = run0 + lane; v < run1; v += 32) {
+        float e[kN];
+        Vec<T>::split(part[v], e);
 #pragma unroll
-            for (int j = 0; j < kN; ++j) most = fmaxf(most, e[j]);
+        for (int j = 0; j < kN; ++j) most = fmaxf(most, e[j]);
+    }
+    const uint32_t my_top = key_of(most);
+    const uint32_t want = k != 0xffffffffu ? k : (uint32_t)kList / 2;  // tokens that the bound has to let through
+    uint32_t warp_bound = 0xffffffffu, reach = 0;  // bound, and how many of the warp's lanes it is known to let through
+    {
+        uint32_t warps = 0;  // of the cluster, with a run
+        for (uint32_t i = 0; i < blocks; ++i) {
+            const int n = min(per, n_vec - (int)i * per);
+            if (n > 0) warps += (uint32_t)((n + chunk - 1) / chunk);
+        }
+        const uint32_t r = (want + want / 4 + warps - 1) / warps;  // a fifth of the warps may have too little to help
+        if (r <= 32) {
+            uint32_t left = my_top, got = 0;
+            while (got < r) {  // the largest that remain, all equal ones at once
+                const uint32_t m = __reduce_max_sync(~0u, left);
+                if (m == kEmptyKey) break;
+                got += __popc(__ballot_sync(~0u, left == m));
+                if (left == m) left = 0;
+                warp_bound = m;
+            }
+            if (got >= r) reach = r;
+            else warp_bound = 0xffffffffu;
         }
     }
-    if (!fine)  // never expected: a second bounded wait, so that no copy outlives the block's shared memory
-        for (int i = 0; i < kPieces; ++i) wait_piece(i);
-    const uint32_t my_top = key_of(most);
 
-    // sums over the cluster; the calling block's predecessors' into `before`
+    // sums and maxima over the cluster
     int turn = 0;
-    auto exchange = [&](Tally v, Tally* before) {
+    auto exchange = [&](Sums v, Sums* before) {  // the blocks' before this one into `before`
 #pragma unroll
-        for (int off = 16; off > 0; off >>= 1) v = join(v, shuffled(v, off));
+        for (int off = 16; off > 0; off >>= 1) {
+            v.a += __shfl_xor_sync(~0u, v.a, off);
+            v.b += __shfl_xor_sync(~0u, v.b, off);
+            v.c += __shfl_xor_sync(~0u, v.c, off);
+        }
+        v.n = __reduce_add_sync(~0u, v.n);
         if (lane == 0) sm.warp[wid] = v;
         __syncthreads();
-        v = sm.warp[lane & (kWarps - 1)];
-#pragma unroll
-        for (int off = kWarps / 2; off > 0; off >>= 1) v = join(v, shuffled(v, off));
-        if (blocks == 1) {
-            if (before) *before = Tally{0, 0, 0, 0};
-            __syncthreads();
-            return v;
+        Sums mine = {0, 0, 0, 0};
+#pragma unroll 4
+        for (int i = 0; i < kWarps; ++i) {
+            const Sums w = sm.warp[i];
+            mine = Sums{mine.a + w.a, mine.b + w.b, mine.c + w.c, mine.n + w.n};
         }
         if (tid < (int)blocks) {  // to every block of the cluster
             const uint32_t to = remote(smem_u32(&sm.peers[turn][rank]), tid);
-            remote_store(to, v.a);
-            remote_store(to + 8, v.b);
-            remote_store(to + 16, (uint64_t)v.top << 32 | v.n);
+            remote_store(to, mine.a);
+            remote_store(to + 8, mine.b);
+            remote_store(to + 16, mine.c);
+            remote_store(to + 24, mine.n);
         }
         __syncwarp();
-        cluster_sync();
-        Tally all = {0, 0, 0, 0}, b = {0, 0, 0, 0};
+        if (blocks > 1) cluster_sync();
+        else __syncthreads();
+        Sums all = {0, 0, 0, 0};
         for (uint32_t i = 0; i < blocks; ++i) {
-            if (i == rank) b = all;
-            all = join(all, sm.peers[turn][i]);
+            if (before && i == rank) *before = all;
+            const Sums w = sm.peers[turn][i];
+            all = Sums{all.a + w.a, all.b + w.b, all.c + w.c, all.n + w.n};
         }
-        if (before) *before = b;
         turn ^= 1;
         return all;
     };
-    const Tally first = exchange(Tally{0, 0, fine ? 0u : 1u, my_top}, nullptr);
-    const uint32_t top_key = first.top;
+    auto exchange_words = [&](Words v) {
+        v.top = __reduce_max_sync(~0u, v.top);
+        v.high = __reduce_max_sync(~0u, v.high);
+        v.n = __reduce_add_sync(~0u, v.n);
+        if (lane == 0) sm.warp_words[wid] = v;
+        __syncthreads();
+        const Words w = sm.warp_words[lane & (kWarps - 1)];
+        v.top = __reduce_max_sync(~0u, w.top);
+        v.high = __reduce_max_sync(~0u, w.high);
+        v.n = __reduce_add_sync(~0u, lane < kWarps ? w.n : 0u);
+        if (tid < (int)blocks) {
+            const uint32_t to = remote(smem_u32(&sm.peer_words[turn][rank]), tid);
+            remote_store32(to, v.top);
+            remote_store32(to + 4, v.high);
+            remote_store32(to + 8, v.n);
+        }
+        __syncwarp();
+        if (blocks > 1) cluster_sync();
+        else __syncthreads();
+        v = Words{0, 0, 0};
+        for (uint32_t i = 0; i < blocks; ++i) {
+            const Words p = sm.peer_words[turn][i];
+            v = Words{max(v.top, p.top), max(v.high, p.high), v.n + p.n};
+        }
+        turn ^= 1;
+        return v;
+    };
     auto answer = [&](int token, uint32_t w, uint64_t mass, uint32_t kept) {
         P.token[row] = token;
-        if (P.logprob) P.logprob[row] = w == 0 ? (mass == 0 ? NAN : -INFINITY) : (float)log((double)w / (double)mass);
+        if (P.logprob) P.logprob[row] = w == 0 ? (mass == 0 ? NAN : -INFINITY) : log_share(w, mass);
         if (P.n_kept) P.n_kept[row] = (int32_t)kept;
     };
-    if (top_key == kEmptyKey || first.n > 0) {  // nothing to draw, or (never expected) a wait that ran out
-        if (rank == 0 && tid == 0) answer(-1, 0, first.n > 0 ? 0 : 1, 0);
+    // the bound's complement, so that the smallest is the maximum; a wait that ran out shows in the count
+    const Words first = exchange_words(Words{my_top, ~warp_bound, (lane == 0 ? reach : 0u) + (fine ? 0u : 1u << 20)});
+    const uint32_t top_key = first.top;
+    if (top_key == kEmptyKey || first.n >= 1u << 20) {  // nothing to draw, or (never expected) a wait that ran out
+        if (rank == 0 && tid == 0) answer(-1, 0, first.n >= 1u << 20 ? 0 : 1, 0);
         return;
     }
+    // a key that at least `want` logits of the row reach, or all of them where there are not so many known to
+    const uint32_t bound = k == 1 ? top_key : first.n >= want ? ~first.high : 1u;
     Scale s;
     s.top = value_of(top_key);
     s.rate = greedy ? 1.f : fminf(__fdiv_rn(0x1.715476p+0f, temperature), 3e38f);
     s.mz = P.minus_zeros;
 
-    // f(two logits, their weights, index of the first) over this block's part; a part's vectors go round the threads
+    // f(two logits, their exponents, index of the first) over this warp's run
     auto each_pair = [&](auto&& f) {
-        for (int v = tid; v < count; v += kThreads) {
+        for (int v = run0 + lane; v < run1; v += 32) {
             float e[kN];
             Vec<T>::split(part[v], e);
 #pragma unroll
@@ -342,82 +429,86 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         }
     };
 
-    // ---- the whole row's mass, and what min-p keeps of it, where no small top-k makes them needless
-    const bool by_list = k <= (uint32_t)kList;
-    uint64_t mass = 0;
+    // ---- without top-k: the row's mass, what min-p keeps of it, and what may stand before that in the order
     bool cut = k != 0xffffffffu || p_part < 0x80000000u;
-    if (!by_list && k == 0xffffffffu && cut) {
-        // Weights fall with the logits but for the rounding of the polynomial: `loose` is below every weight that can
-        // stand before one of `least` in the order.
-        const uint32_t loose = least - min(least, (least >> 20) + 1u);
-        Tally v = {0, 0, 0, 0};
-        each_pair([&](float, float, float y0, float y1, int) {
-            uint32_t w0, w1;
-            weights(s, y0, y1, w0, w1);
-            v.a += (uint64_t)w0 + w1;
-            v.b += (uint64_t)(w0 >= loose ? w0 : 0u) + (w1 >= loose ? w1 : 0u);
-        });
-        v = exchange(v, nullptr);
-        mass = v.a;
+    uint64_t mass = 0;
+    Sums kept = {0, 0, 0, 0}, kept_before = {0, 0, 0, 0};  // c: mass kept, n: tokens kept
+    if (k == 0xffffffffu) {
+        Sums v = {0, 0, 0, 0};
+        if (least == 1) {
+            each_pair([&](float, float, float y0, float y1, int) {
+                uint32_t w0, w1;
+                weights(s, y0, y1, w0, w1);
+                v.a += (uint64_t)w0 + w1;
+                v.n += min(w0, 1u) + min(w1, 1u);
+            });
+            v.c = v.a;
+        } else {
+            // Weights fall with the logits but for the rounding of the polynomial: `loose` is below every weight that
+            // can stand before one of `least` in the order.
+            const uint32_t loose = least - min(least, (least >> 20) + 1u);
+            each_pair([&](float, float, float y0, float y1, int) {
+                uint32_t w0, w1;
+                weights(s, y0, y1, w0, w1);
+                v.a += (uint64_t)w0 + w1;
+                if (max(w0, w1) < loose) return;
+                v.b += (uint64_t)(w0 >= loose ? w0 : 0u) + (w1 >= loose ? w1 : 0u);
+                v.c += (uint64_t)(w0 >= least ? w0 : 0u) + (w1 >= least ? w1 : 0u);
+                v.n += (w0 >= least) + (w1 >= least);
+            });
+        }
+        kept = exchange(v, &kept_before);
+        if (lane == 0) sm.warp_mass[wid] = sm.warp[wid].c;
+        mass = kept.a;
         // every token that min-p keeps comes before the nucleus ends
-        if (least > 1 && v.b <= share_of(mass, p_part)) cut = false;
+        if (cut && least > 1 && kept.b <= share_of(mass, p_part)) cut = false;
     }
 
     // ---- few tokens: candidates to the first block
-    if (cut && (by_list || k == 0xffffffffu)) {
-        const uint32_t want = by_list ? k : (uint32_t)kList;
-        // the largest bound (of the upper key bits) that `want` threads' maxima reach; 1 where there are not so many
-        uint32_t lo = 0, hi = top_key >> 16;
-        while (lo < hi) {
-            const uint32_t mid = hi - (hi - lo) / 2;
-            if ((uint32_t)__syncthreads_count(my_top >> 16 >= mid) >= want) lo = mid;
-            else hi = mid - 1;
-        }
-        const uint32_t bound = max(lo << 16, 1u);
-        if (my_top >= bound) {
-            for (int v = tid; v < count; v += kThreads) {
-                float e[kN];
-                Vec<T>::split(part[v], e);
-#pragma unroll
-                for (int j = 0; j < kN; ++j) {
-                    const uint32_t key = key_of(e[j]);
-                    if (key >= bound) {
-                        const uint32_t at = atomicAdd(&sm.n_mine, 1u);
-                        if (at < kMine) sm.mine[at] = (uint64_t)key << 32 | (uint32_t)~(base + v * kN + j);
-                    }
+    if (cut && want <= (uint32_t)kList) {
+        const uint32_t share = kGather / blocks, to = remote(smem_u32(sm.gather), 0) + 8 * rank * share;
+        for (uint32_t m = __ballot_sync(~0u, my_top >= bound); m; m &= m - 1) {  // the logits of a lane that reaches it
+            const int of = __ffs(m) - 1, n = (run1 - run0 - of + 31) / 32 * kN;
+            for (int i = lane; i < n; i += 32) {
+                const int at = (run0 + of + i / kN * 32) * kN + i % kN;
+                const uint32_t key = key_of(to_float(reinterpret_cast<const T*>(part)[at]));
+                if (key >= bound) {
+                    const uint32_t slot = atomicAdd(&sm.n_mine, 1u);
+                    if (slot < share) remote_store(to + 8 * slot, (uint64_t)key << 32 | (uint32_t)~(base + at));
                 }
             }
+            __syncwarp();
         }
         __syncthreads();
-        const uint32_t n_mine = sm.n_mine;
-        Tally before;
-        const uint32_t n = exchange(Tally{0, 0, tid > 0 ? 0 : n_mine <= kMine ? n_mine : kGather + 1, 0}, &before).n;
-        const bool fits = n <= kGather;  // known to every block
-        if (fits) {
-            const uint32_t to = remote(smem_u32(sm.gather), 0) + 8 * before.n;
-            for (uint32_t i = tid; i < n_mine; i += kThreads) remote_store(to + 8 * i, sm.mine[i]);
-            __syncwarp();
-            cluster_sync();
-            if (by_list && rank != 0) return;
-        }
-        uint32_t done = 0;  // 1: the first block has the token
-        if (rank == 0 && fits) {
-            // the first `want` of them: those not below the want-th
-            uint64_t mine[kGather / kThreads];
+        if (tid < (int)blocks) remote_store32(remote(smem_u32(&sm.counts[rank]), tid), sm.n_mine);
+        __syncwarp();
+        if (blocks > 1) cluster_sync();
+        else __syncthreads();
+        bool fits = true;
+        for (uint32_t i = 0; i < blocks; ++i) fits = fits && sm.counts[i] <= share;
+        if (fits && k != 0xffffffffu && rank != 0) return;
+        bool done = false;  // the first block has the token
+        if (fits && rank == 0) {
+            for (uint32_t i = tid; i < blocks * share; i += kThreads)
+                if (i % share < sm.counts[i / share]) sm.list[atomicAdd(&sm.n_list, 1u)] = sm.gather[i];
+            __syncthreads();
+            const uint32_t n = sm.n_list;
+            constexpr int kOwn = kGather / kThreads;
+            uint64_t own[kOwn];
 #pragma unroll
-            for (int i = 0; i < kGather / kThreads; ++i) mine[i] = tid + i * kThreads < (int)n ? sm.gather[tid + i * kThreads] : 0;
+            for (int i = 0; i < kOwn; ++i) own[i] = tid + i * kThreads < (int)n ? sm.list[tid + i * kThreads] : 0;
+            // the first `want` of them: those not below the want-th
             uint64_t last = 1;
             if (n > want) {
-                uint64_t a = 1, b = (uint64_t)top_key << 32 | 0xffffffffu;
+                uint64_t a = (uint64_t)bound << 32, b = (uint64_t)top_key << 32 | 0xffffffffu;
                 while (a < b) {
                     const uint64_t mid = b - (b - a) / 2;
                     int c = 0;
 #pragma unroll
-                    for (int i = 0; i < kGather / kThreads; ++i) c += mine[i] >= mid;
-                    // a count of threads is at most the count; more than one of a thread's are counted one by one
+                    for (int i = 0; i < kOwn; ++i) c += own[i] >= mid;
                     uint32_t total = __syncthreads_count(c > 0);
 #pragma unroll
-                    for (int i = 1; i < kGather / kThreads; ++i)
+                    for (int i = 1; i < kOwn; ++i)
                         if (n > (uint32_t)(i * kThreads)) total += __syncthreads_count(c > i);
                     if (total >= want) a = mid;
                     else b = mid - 1;
@@ -426,77 +517,86 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
                 last = a;
             }
             __syncthreads();
-            if (tid == 0) sm.n_mine = 0;
+            if (tid == 0) sm.n_list = 0;
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < kGather / kThreads; ++i)
-                if (mine[i] >= last) sm.mine[atomicAdd(&sm.n_mine, 1u) & (kMine - 1)] = mine[i];
+            for (int i = 0; i < kOwn; ++i)
+                if (own[i] >= last) sm.list[atomicAdd(&sm.n_list, 1u)] = own[i];
             __syncthreads();
-            const uint32_t m = min(sm.n_mine, (uint32_t)kList);
-            // a thread a token, in no order: ranks and sums by comparison with every other
-            uint64_t* ws = reinterpret_cast<uint64_t*>(sm.bins);
-            const uint64_t me = tid < (int)m ? sm.mine[tid] : 0;
+            // `team` threads a token, in no order: sums by comparison with every other token
+            const uint32_t m = sm.n_list;  // <= want
+            int team_log2 = 1;
+            while (team_log2 < 5 && (m << (team_log2 + 1)) <= kThreads) ++team_log2;
+            const uint32_t team = 1u << team_log2, i_me = (uint32_t)tid >> team_log2, j0 = (uint32_t)tid & (team - 1);
+            const uint64_t me = i_me < m ? sm.list[i_me] : 0;
             const uint32_t index = ~(uint32_t)me;
-            uint32_t w = tid < (int)m ? weight_of(s, value_of((uint32_t)(me >> 32))) : 0;
-            if (tid < kList) ws[tid] = w;
+            uint32_t* ws = &sm.bins[0][0];
+            uint32_t w = i_me < m ? weight_of(s, value_of((uint32_t)(me >> 32))) : 0;
+            if (j0 == 0 && i_me < m) ws[i_me] = w;
             __syncthreads();
             uint64_t above = 0, sum = 0;
-            if (tid < (int)m)
-                for (uint32_t j = 0; j < m; ++j) {
-                    const uint64_t wj = ws[j];
-                    sum += wj;
-                    above += sm.mine[j] > me ? wj : 0;
-                }
-            const uint64_t goal = p_part < 0x80000000u ? share_of(by_list ? sum : mass, p_part) : ~0ull;
+#pragma unroll 4
+            for (uint32_t j = j0; j < m; j += team) {
+                const uint32_t wj = ws[j];
+                sum += wj;
+                above += sm.list[j] > me ? wj : 0u;
+            }
+            for (uint32_t off = 1; off < team; off <<= 1) {
+                sum += __shfl_xor_sync(~0u, sum, off);
+                above += __shfl_xor_sync(~0u, above, off);
+            }
+            const uint64_t goal = p_part < 0x80000000u ? share_of(k != 0xffffffffu ? sum : mass, p_part) : ~0ull;
             // the nucleus ends among them, or they are all there is
-            const bool enough = by_list || n < want || __syncthreads_or(tid < (int)m && above + w >= goal);
+            const bool enough = k != 0xffffffffu || n < want || __syncthreads_or(i_me < m && above + w >= goal);
             if (!(above < goal || above == 0) || w < least) w = 0;
             __syncthreads();
-            if (tid < kList) ws[tid] = w;
-            const uint32_t kept = __syncthreads_count(w > 0);
+            if (j0 == 0 && i_me < m) ws[i_me] = w;
+            const uint32_t n_kept = __syncthreads_count(w > 0 && j0 == 0 && i_me < m);
             if (enough) {
                 uint64_t before = 0;
                 sum = 0;
-                if (w > 0)
-                    for (uint32_t j = 0; j < m; ++j) {
-                        const uint64_t wj = ws[j];
-                        sum += wj;
-                        before += ~(uint32_t)sm.mine[j] < index ? wj : 0;
-                    }
+#pragma unroll 4
+                for (uint32_t j = j0; j < m; j += team) {
+                    const uint32_t wj = ws[j];
+                    sum += wj;
+                    before += ~(uint32_t)sm.list[j] < index ? wj : 0u;
+                }
+                for (uint32_t off = 1; off < team; off <<= 1) {
+                    sum += __shfl_xor_sync(~0u, sum, off);
+                    before += __shfl_xor_sync(~0u, before, off);
+                }
                 const uint64_t at_mass = share_of(sum, u_part);
-                if (w > 0 && before <= at_mass && at_mass < before + w) answer((int)index, w, sum, kept);
-                done = 1;
+                if (j0 == 0 && i_me < m && w > 0 && before <= at_mass && at_mass < before + w) answer((int)index, w, sum, n_kept);
+                done = true;
             }
         }
-        if (by_list && fits) return;
-        if (fits && exchange(Tally{0, 0, 0, done}, nullptr).top) return;
+        if (fits && (k != 0xffffffffu || exchange_words(Words{done ? 1u : 0u, 0, 0}).top)) return;
     }
 
     // ---- the cut: keys above cut_key, and those equal to it up to cut_index
     uint32_t cut_key = 1;
     int cut_index = P.vocab;
     auto in_cut = [&](uint32_t key, int i) { return key > cut_key || (key == cut_key && i <= cut_index); };
-    // moves the cut to the first tokens of the order that reach `count` tokens or `goal`
-    auto cut_at = [&](uint32_t n_goal, uint64_t goal) {
+    // moves the cut to the first tokens of the order that reach `n_goal` tokens or the mass `goal`, all of whose keys
+    // are at least `floor`
+    auto cut_at = [&](uint32_t n_goal, uint64_t goal, uint32_t floor) {
         uint64_t over = 0;      // mass and count above the part of a bin that the cut lies in
         uint32_t n_over = 0;
-        uint32_t lo_key = cut_key, hi_key = top_key;
-        int from = 0;           // in units of the level
-        bool reached = true;
-        for (int level = 0; level < 2 && reached; ++level) {
+        int from = 0;           // the part, in units of the level
+        for (int level = 0; level < 2; ++level) {
             const float unit = level == 0 ? 16.f : 16.f * kBins;  // bins of y a unit
             for (int i = tid; i < 3 * kBins; i += kThreads) (&sm.bins[0][0])[i] = 0;
             __syncthreads();
             each_pair([&](float x0, float x1, float y0, float y1, int at) {
-                uint32_t w[2];
                 const float y[2] = {y0, y1}, e[2] = {x0, x1};
+                uint32_t w[2];
                 int bin[2];
                 bool in[2];
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     bin[j] = (int)(-y[j] * unit) - from;
                     const uint32_t key = key_of(e[j]);
-                    in[j] = key != kEmptyKey && in_cut(key, at + j) && bin[j] >= 0 && (level == 0 || bin[j] < kBins || from == (kBins - 1) * kBins);
+                    in[j] = key >= floor && in_cut(key, at + j) && bin[j] >= 0 && (level == 0 || bin[j] < kBins || from == (kBins - 1) * kBins);
                     bin[j] = min(bin[j], kBins - 1);
                 }
                 if (!in[0] && !in[1]) return;
@@ -527,7 +627,10 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
                 const uint32_t b = __shfl_up_sync(~0u, cs, off);
                 if (lane >= off) ms += a, cs += b;
             }
-            if (lane == 31) sm.warp[wid] = Tally{ms, 0, cs, 0};
+            if (lane == 31) {
+                sm.warp[wid].a = ms;
+                sm.warp[wid].n = cs;
+            }
             if (tid == 0) sm.found[0] = ~0ull;
             __syncthreads();
             ms += over;
@@ -541,22 +644,36 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
             }
             if (blocks > 1) cluster_sync();  // no block clears its bins while another reads them
             else __syncthreads();
-            reached = sm.found[0] != ~0ull;
-            if (reached) {
-                over = sm.found[1];
-                n_over = (uint32_t)sm.found[2];
-                from = level == 0 ? (int)sm.found[0] * kBins : from + (int)sm.found[0];
-            }
+            if (sm.found[0] == ~0ull) return;  // the goal is beyond all of them
+            over = sm.found[1];
+            n_over = (uint32_t)sm.found[2];
+            from = level == 0 ? (int)sm.found[0] * kBins : from + (int)sm.found[0];
             __syncthreads();
         }
-        if (!reached) return;  // the goal is beyond all of them
         const bool last_bin = from == kBins * kBins - 1;  // open to below
         auto in_part = [&](float y) {
             const int b = (int)(-y * (16.f * kBins));
             return last_bin ? b >= from : b == from;
         };
+        // the part's largest and smallest key
+        uint32_t low = 0xffffffffu, high = 0;
+        each_pair([&](float x0, float x1, float y0, float y1, int at) {
+            const float y[2] = {y0, y1}, e[2] = {x0, x1};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                if (!in_part(y[j])) continue;
+                const uint32_t key = key_of(e[j]);
+                if (key >= floor && in_cut(key, at + j)) {
+                    low = min(low, key);
+                    high = max(high, key);
+                }
+            }
+        });
+        const Words ends = exchange_words(Words{high, ~low, 0});
+        uint32_t hi_key = ends.top, lo_key = ~ends.high;
+        Sums v = {0, 0, 0, 0};
         auto tally_part = [&](uint32_t from_key) {  // the part's keys >= from_key
-            Tally v = {0, 0, 0, 0};
+            Sums t = {0, 0, 0, 0};
             each_pair([&](float x0, float x1, float y0, float y1, int at) {
                 const float y[2] = {y0, y1}, e[2] = {x0, x1};
                 if (!in_part(y0) && !in_part(y1)) return;
@@ -565,163 +682,124 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const uint32_t key = key_of(e[j]);
-                    if (key != kEmptyKey && key >= from_key && in_part(y[j]) && in_cut(key, at + j))
-                        v = join(v, Tally{w[j], 0, 1, key});
+                    if (key >= from_key && key >= floor && in_part(y[j]) && in_cut(key, at + j)) {
+                        t.a += w[j];
+                        t.n += 1;
+                    }
                 }
             });
-            return v;
+            return exchange(t, nullptr);
         };
-        // the part's largest and smallest key
-        Tally v = tally_part(1);
-        uint32_t low = 0xffffffffu;
-        each_pair([&](float x0, float x1, float y0, float y1, int at) {
-            const float y[2] = {y0, y1}, e[2] = {x0, x1};
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const uint32_t key = key_of(e[j]);
-                if (key != kEmptyKey && in_part(y[j]) && in_cut(key, at + j)) low = min(low, key);
+        if (lo_key < hi_key) {
+            while (lo_key < hi_key) {
+                const uint32_t mid = hi_key - (hi_key - lo_key) / 2;
+                v = tally_part(mid);
+                if (n_over + v.n >= n_goal || over + v.a >= goal) lo_key = mid;
+                else hi_key = mid - 1;
             }
-        });
-        hi_key = exchange(Tally{0, 0, 0, v.top}, nullptr).top;
-        lo_key = ~exchange(Tally{0, 0, 0, ~low}, nullptr).top;
-        while (lo_key < hi_key) {
-            const uint32_t mid = hi_key - (hi_key - lo_key) / 2;
-            v = exchange(tally_part(mid), nullptr);
-            if (n_over + v.n >= n_goal || over + v.a >= goal) lo_key = mid;
-            else hi_key = mid - 1;
+            v = tally_part(lo_key + 1);
         }
         // of the tokens equal to it, those still needed, by index
-        v = lo_key == 0xffffffffu ? Tally{0, 0, 0, 0} : exchange(tally_part(lo_key + 1), nullptr);
         const uint32_t w = weight_of(s, value_of(lo_key));
         uint64_t need = n_goal - n_over - v.n;
         if (goal != ~0ull) {
             const uint64_t by_mass = w > 0 ? (goal - over - v.a + w - 1) / w : ~0ull;
             need = by_mass < need ? by_mass : need;
         }
-        // a contiguous run of vectors to a thread
-        const int run = (count + kThreads - 1) / kThreads, a0 = min(tid * run, count), a1 = min(a0 + run, count);
         uint32_t c = 0;
-        for (int i = a0 * kN; i < a1 * kN; ++i) {
-            const uint32_t key = key_of(to_float(reinterpret_cast<const T*>(part)[i]));
-            c += key == lo_key && in_cut(key, base + i);
-        }
-        Tally before;
-        exchange(Tally{0, 0, c, 0}, &before);
-        uint32_t cs = c;
-#pragma unroll
-        for (int off = 1; off < 32; off <<= 1) {
-            const uint32_t b = __shfl_up_sync(~0u, cs, off);
-            if (lane >= off) cs += b;
-        }
-        if (lane == 31) sm.warp[wid].n = cs;
-        __syncthreads();
-        for (int i = 0; i < wid; ++i) cs += sm.warp[i].n;
-        cs += before.n;
+        each_pair([&](float x0, float x1, float, float, int at) {
+            c += (key_of(x0) == lo_key && in_cut(lo_key, at)) + (key_of(x1) == lo_key && in_cut(lo_key, at + 1));
+        });
+        c = __reduce_add_sync(~0u, c);
+        Sums before;
+        exchange(Sums{0, 0, 0, lane == 0 ? c : 0u}, &before);
+        uint64_t seen = before.n;  // by the warps before this one
+        for (int i = 0; i < wid; ++i) seen += sm.warp[i].n;
         uint32_t index = 0;
-        if (cs - c < need && need <= cs) {
-            uint64_t left = need - (cs - c);
-            for (int i = a0 * kN; i < a1 * kN; ++i) {
-                const uint32_t key = key_of(to_float(reinterpret_cast<const T*>(part)[i]));
-                if (key == lo_key && in_cut(key, base + i) && --left == 0) {
-                    index = (uint32_t)(base + i) + 1u;
-                    break;
+        if (seen < need && need <= seen + c) {  // in this warp's run: 32 logits at a time
+            for (int i = run0 * kN; i < run1 * kN; i += 32) {
+                const uint32_t key = i + lane < run1 * kN ? key_of(to_float(reinterpret_cast<const T*>(part)[i + lane])) : 0;
+                uint32_t m = __ballot_sync(~0u, key == lo_key && in_cut(key, base + i + lane));
+                if (seen + __popc(m) < need) {
+                    seen += __popc(m);
+                    continue;
                 }
+                for (; seen + 1 < need; ++seen) m &= m - 1;
+                index = (uint32_t)(base + i + __ffs(m));  // one past it
+                break;
             }
         }
-        __syncthreads();
-        index = exchange(Tally{0, 0, 0, index}, nullptr).top;
+        cut_index = (int)exchange_words(Words{index, 0, 0}).top - 1;  // the goal is reached, so that there is one
         cut_key = lo_key;
-        cut_index = (int)index - 1;  // the goal is reached, so that there is one
     };
     if (cut) {
-        if (k != 0xffffffffu) {
-            cut_at(k, ~0ull);
-            if (p_part < 0x80000000u) {
-                Tally v = {0, 0, 0, 0};
+        if (k != 0xffffffffu) cut_at(k, ~0ull, bound);
+        if (p_part < 0x80000000u) {
+            if (k != 0xffffffffu) {
+                Sums v = {0, 0, 0, 0};
                 each_pair([&](float x0, float x1, float y0, float y1, int at) {
+                    const bool in0 = in_cut(key_of(x0), at), in1 = in_cut(key_of(x1), at + 1);
+                    if (!in0 && !in1) return;
                     uint32_t w0, w1;
                     weights(s, y0, y1, w0, w1);
-                    v.a += (uint64_t)(in_cut(key_of(x0), at) ? w0 : 0u) + (in_cut(key_of(x1), at + 1) ? w1 : 0u);
+                    v.a += (uint64_t)(in0 ? w0 : 0u) + (in1 ? w1 : 0u);
                 });
                 mass = exchange(v, nullptr).a;
             }
-        }
-        if (p_part < 0x80000000u) {
             const uint64_t goal = share_of(mass, p_part);
-            cut_at(0xffffffffu, goal > 0 ? goal : 1);
+            cut_at(0xffffffffu, goal > 0 ? goal : 1, cut_key);
         }
+        Sums v = {0, 0, 0, 0};
+        each_pair([&](float x0, float x1, float y0, float y1, int at) {
+            const bool in0 = in_cut(key_of(x0), at), in1 = in_cut(key_of(x1), at + 1);
+            if (!in0 && !in1) return;
+            uint32_t w0, w1;
+            weights(s, y0, y1, w0, w1);
+            if (!in0 || w0 < least) w0 = 0;
+            if (!in1 || w1 < least) w1 = 0;
+            v.c += (uint64_t)w0 + w1;
+            v.n += min(w0, 1u) + min(w1, 1u);
+        });
+        kept = exchange(v, &kept_before);
+        if (lane == 0) sm.warp_mass[wid] = sm.warp[wid].c;
     }
 
-    // ---- the draw: every block's kept mass, then the token in the block that holds it
-    auto kept_weights = [&](float x0, float x1, int at, uint32_t& w0, uint32_t& w1) {
-        float y0, y1;
-        exponents(s, x0, x1, y0, y1);
-        weights(s, y0, y1, w0, w1);
-        if (w0 < least || (cut && !in_cut(key_of(x0), at))) w0 = 0;
-        if (w1 < least || (cut && !in_cut(key_of(x1), at + 1))) w1 = 0;
+    // ---- the draw: the warp's run that holds it, shared out over the block
+    const uint64_t goal = share_of(kept.c, u_part);
+    __syncthreads();
+    uint64_t run_begin = kept_before.c;
+    int run = 0;
+    if (goal < run_begin) return;
+    for (; run < kWarps && goal >= run_begin + sm.warp_mass[run]; ++run) run_begin += sm.warp_mass[run];
+    if (run == kWarps) return;  // in a later block's part
+    const int e0 = run * chunk * kN, e1 = min((run + 1) * chunk, count) * kN;
+    const int each = (chunk * kN + kThreads - 1) / kThreads, a0 = min(e0 + tid * each, e1), a1 = min(a0 + each, e1);
+    auto kept_weight = [&](int i) {
+        const float v = to_float(reinterpret_cast<const T*>(part)[i]);
+        if (cut && !in_cut(key_of(v), base + i)) return 0u;
+        const uint32_t w = weight_of(s, v);
+        return w >= least ? w : 0u;
     };
-    Tally mine = {0, 0, 0, 0};
-    for (int v = tid; v < count; v += kThreads) {
-        float e[kN];
-        Vec<T>::split(part[v], e);
-#pragma unroll
-        for (int j = 0; j < kN; j += 2) {
-            uint32_t w0, w1;
-            kept_weights(e[j], e[j + 1], base + v * kN + j, w0, w1);
-            mine.a += (uint64_t)w0 + w1;
-            mine.n += (w0 > 0) + (w1 > 0);
-        }
-    }
-    Tally before;
-    const uint64_t my_mass = [&] {  // of the block
-        Tally v = mine;
-#pragma unroll
-        for (int off = 16; off > 0; off >>= 1) v = join(v, shuffled(v, off));
-        if (lane == 0) sm.prefix[wid] = v.a;
-        __syncthreads();
-        uint64_t m = 0;
-        for (int i = 0; i < kWarps; ++i) m += sm.prefix[i];
-        __syncthreads();
-        return m;
-    }();
-    const Tally all = exchange(mine, &before);
-    const uint64_t goal = share_of(all.a, u_part);
-    if (goal < before.a || goal >= before.a + my_mass) return;
-    const int run = (count + kThreads - 1) / kThreads, a0 = min(tid * run, count), a1 = min(a0 + run, count);
     uint64_t sum = 0;
-    for (int v = a0; v < a1; ++v) {
-        float e[kN];
-        Vec<T>::split(part[v], e);
-#pragma unroll
-        for (int j = 0; j < kN; j += 2) {
-            uint32_t w0, w1;
-            kept_weights(e[j], e[j + 1], base + v * kN + j, w0, w1);
-            sum += (uint64_t)w0 + w1;
-        }
-    }
+    for (int i = a0; i < a1; ++i) sum += kept_weight(i);
     uint64_t upto = sum;
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
         const uint64_t v = __shfl_up_sync(~0u, upto, off);
         if (lane >= off) upto += v;
     }
-    if (lane == 31) sm.prefix[wid] = upto;
+    if (lane == 31) sm.warp[wid].a = upto;
     __syncthreads();
-    for (int i = 0; i < wid; ++i) upto += sm.prefix[i];
-    uint64_t at_mass = before.a + upto - sum;
+    for (int i = 0; i < wid; ++i) upto += sm.warp[i].a;
+    uint64_t at_mass = run_begin + upto - sum;
     if (at_mass <= goal && goal < at_mass + sum) {
-        for (int v = a0; v < a1; ++v) {
-            float e[kN];
-            Vec<T>::split(part[v], e);
-#pragma unroll
-            for (int j = 0; j < kN; j += 2) {
-                uint32_t w0, w1;
-                kept_weights(e[j], e[j + 1], base + v * kN + j, w0, w1);
-                if (at_mass <= goal && goal < at_mass + w0) answer(base + v * kN + j, w0, all.a, all.n);
-                at_mass += w0;
-                if (at_mass <= goal && goal < at_mass + w1) answer(base + v * kN + j + 1, w1, all.a, all.n);
-                at_mass += w1;
+        for (int i = a0; i < a1; ++i) {
+            const uint32_t w = kept_weight(i);
+            if (goal < at_mass + w) {
+                answer(base + i, w, kept.c, kept.n);
+                break;
             }
+            at_mass += w;
         }
     }
 }
