@@ -51,6 +51,7 @@ __device__ __forceinline__ float to_float(float x) { return x; }
 template <typename T> __device__ __forceinline__ T from_float(float x);
 template <> __device__ __forceinline__ __nv_bfloat16 from_float<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half from_float<__half>(float x) { return __float2half_rn(x); }
+template <> __device__ __forceinline__ float from_float<float>(float x) { return x; }
 // two values in one 32-bit register, the first in the low half; kExpOne: the unit of both exponents
 template <typename T> struct Pair;
 template <> struct Pair<__nv_bfloat16> {

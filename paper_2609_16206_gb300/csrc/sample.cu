@@ -9,10 +9,10 @@
 // copies; everything after is passes over that copy and exchanges of a few
 // words over the cluster.  The kept tokens are the ones before a cut in the
 // order (falling logits, then index):
-//   * few of them (top-k up to kList, or a nucleus that is): each warp's r-th
-//     largest of its lanes' maxima, the smallest of them over the cluster, is a
-//     bound that r logits of every warp reach and few others do; those go to
-//     the first block, which ranks them;
+//   * few of them (top-k up to kList, or a nucleus that is): every warp shows
+//     the largest of its lanes' maxima to the cluster, and the k-th largest of
+//     those is a bound that at least k logits reach and not many more do; those
+//     go to the first block, which ranks them;
 //   * a nucleus cut off by min-p anyway needs no cut: the mass of what min-p
 //     keeps, summed with the whole row's, shows it;
 //   * else the cut is found from the masses (or counts) of 512 bins of y, then
@@ -28,7 +28,7 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kList = 256;          // tokens that the first block ranks
-constexpr int kGather = 1536;       // candidates of the cluster, an equal share of them to a block
+constexpr int kGather = 1024;       // candidates of the cluster, an equal share of them to a block
 constexpr int kBins = 512;
 constexpr int kPieces = 4;          // of a block's part of the row, each a bulk copy
 constexpr uint32_t kEmptyKey = 0;   // of -inf and NaN
@@ -75,10 +75,6 @@ __device__ __forceinline__ void exponents(const Scale& s, float x0, float x1, fl
     const uint64_t y = fma2(add2(pack(x0, x1), pack(-s.top, -s.top)), pack(s.rate, s.rate), s.mz);
     y0 = fmaxf(__uint_as_float((uint32_t)y), -64.f);
     y1 = fmaxf(__uint_as_float((uint32_t)(y >> 32)), -64.f);
-    if (s.top == INFINITY) {  // only the infinite ones have a weight
-        y0 = x0 == INFINITY ? 0.f : -64.f;
-        y1 = x1 == INFINITY ? 0.f : -64.f;
-    }
 }
 
 // round(2^31 2^y): y = k + f with k its nearest integer (by adding 1.5 2^23, whose low bits are then k), 2^f =
@@ -166,12 +162,15 @@ __device__ __forceinline__ uint32_t remote_load(uint32_t addr)
 }
 struct __align__(16) Shared {
     uint64_t gather[kGather];       // first block: (key, ~index) of the candidates
-    uint64_t list[kGather];         // the same without gaps, then the ranked ones'
-    uint32_t bins[3][kBins];        // low and high halves of the masses, counts; the ranked ones' weights
+    uint64_t list[kGather];         // the same without gaps
+    uint32_t weight[kGather];       // theirs
+    uint32_t kept[kGather];         // the same, 0 where not kept
+    uint32_t bins[3][kBins];        // low and high halves of the masses, counts
     Sums warp[kWarps];
     Words warp_words[kWarps];
     Sums peers[2][kMaxCluster];     // exchanges alternate between the two
     Words peer_words[2][kMaxCluster];
+    uint32_t shown[kThreads];       // the largest maxima of every warp of the cluster
     uint64_t warp_mass[kWarps];     // what each warp's run holds of the kept tokens
     uint64_t found[3];
     uint32_t counts[kMaxCluster];   // candidates of each block
@@ -300,7 +299,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     float most = -INFINITY;
     // (a block leaves only after every piece has landed: each has warps that wait for it, and the exchange is behind
     // them; a wait that runs out, never expected, is given a second bound for that and spoils the row)
-    const bool fine = wait_piece(wid / (kWarps / kPieces));
+    bool fine = wait_piece(wid / (kWarps / kPieces));
+    fine = __all_sync(~0u, fine);
     if (!fine) wait_piece(wid / (kWarps / kPieces));
     for (int v = run0 + lane; v < run1; v += 32) {
         float e[kN];
@@ -308,29 +308,33 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
 #pragma unroll
         for (int j = 0; j < kN; ++j) most = fmaxf(most, e[j]);
     }
-    const uint32_t my_top = key_of(most);
+    uint32_t my_top = key_of(most);
     const uint32_t want = k != 0xffffffffu ? k : (uint32_t)kList / 2;  // tokens that the bound has to let through
-    uint32_t warp_bound = 0xffffffffu, reach = 0;  // bound, and how many of the warp's lanes it is known to let through
+    // so many of each warp that the cluster's are a few times as many as wanted; a place for each of a block's threads
+    const uint32_t places = kThreads / (kWarps * blocks);
+    const uint32_t show = min(places, (3 * min(want, (uint32_t)kThreads) + kWarps * blocks - 1) / (kWarps * blocks));
     {
-        uint32_t warps = 0;  // of the cluster, with a run
-        for (uint32_t i = 0; i < blocks; ++i) {
-            const int n = min(per, n_vec - (int)i * per);
-            if (n > 0) warps += (uint32_t)((n + chunk - 1) / chunk);
+        uint32_t left = my_top, mine = 0;  // lane i: the i-th largest
+        for (uint32_t i = 0; i < show; ++i) {
+            const uint32_t m = __reduce_max_sync(~0u, left);
+            if (lane == (int)i) mine = m;
+            if (lane == __ffs(__ballot_sync(~0u, left == m)) - 1) left = 0;
         }
-        const uint32_t r = (want + want / 4 + warps - 1) / warps;  // a fifth of the warps may have too little to help
-        if (r <= 32) {
-            uint32_t left = my_top, got = 0;
-            while (got < r) {  // the largest that remain, all equal ones at once
-                const uint32_t m = __reduce_max_sync(~0u, left);
-                if (m == kEmptyKey) break;
-                got += __popc(__ballot_sync(~0u, left == m));
-                if (left == m) left = 0;
-                warp_bound = m;
-            }
-            if (got >= r) reach = r;
-            else warp_bound = 0xffffffffu;
+        // (a wait that ran out shows as a key that no logit has)
+        if (!fine) mine = 0xffffffffu;
+        for (uint32_t i = lane; i < places * blocks; i += 32) {
+            const uint32_t v = __shfl_sync(~0u, mine, i / blocks);
+            remote_store32(remote(smem_u32(&sm.shown[(rank * kWarps + wid) * places + i / blocks]), i % blocks), v);
         }
     }
+    __syncwarp();
+    if (blocks > 1) cluster_sync();
+    else __syncthreads();
+    const uint32_t shown = sm.shown[tid];
+    uint32_t top_key = __reduce_max_sync(~0u, shown);
+    if (lane == 0) sm.warp_words[wid].top = top_key;
+    __syncthreads();
+    top_key = __reduce_max_sync(~0u, sm.warp_words[lane & (kWarps - 1)].top);
 
     // sums and maxima over the cluster
     int turn = 0;
@@ -401,15 +405,45 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         if (P.logprob) P.logprob[row] = w == 0 ? (mass == 0 ? NAN : -INFINITY) : log_share(w, mass);
         if (P.n_kept) P.n_kept[row] = (int32_t)kept;
     };
-    // the bound's complement, so that the smallest is the maximum; a wait that ran out shows in the count
-    const Words first = exchange_words(Words{my_top, ~warp_bound, (lane == 0 ? reach : 0u) + (fine ? 0u : 1u << 20)});
-    const uint32_t top_key = first.top;
-    if (top_key == kEmptyKey || first.n >= 1u << 20) {  // nothing to draw, or (never expected) a wait that ran out
-        if (rank == 0 && tid == 0) answer(-1, 0, first.n >= 1u << 20 ? 0 : 1, 0);
+    if (top_key == kEmptyKey || top_key == 0xffffffffu) {  // nothing to draw, or (never expected) a wait that ran out
+        if (rank == 0 && tid == 0) answer(-1, 0, top_key == kEmptyKey ? 1 : 0, 0);
         return;
     }
-    // a key that at least `want` logits of the row reach, or all of them where there are not so many known to
-    const uint32_t bound = k == 1 ? top_key : first.n >= want ? ~first.high : 1u;
+    const bool infinite = top_key == key_of(INFINITY);
+    if (infinite) {  // only the infinite logits have a weight: as zeros, the others as -inf
+        for (int i = run0 * kN + lane; i < run1 * kN; i += 32) {
+            T* at = reinterpret_cast<T*>(part) + i;
+            *at = from_float<T>(to_float(*at) == INFINITY ? 0.f : -INFINITY);
+        }
+        __syncwarp();
+        most = -INFINITY;
+        for (int v = run0 + lane; v < run1; v += 32) {
+            float e[kN];
+            Vec<T>::split(part[v], e);
+#pragma unroll
+            for (int j = 0; j < kN; ++j) most = fmaxf(most, e[j]);
+        }
+        my_top = key_of(most);
+        top_key = key_of(0.f);
+    }
+    // A key that at least `want` logits of the row reach: the want-th largest of the shown; 1 where not so many are.
+    uint32_t bound = top_key;
+    if (k > 1 && !infinite) {
+        // from the warps' own maxima, if they are enough, to an eighth more than wanted or keys 2^12 near (2^-11 of a
+        // logit)
+        uint32_t low = __reduce_min_sync(~0u, tid % places == 0 ? shown : 0xffffffffu), hi = top_key;
+        if (lane == 0) sm.warp_words[wid].high = low;
+        __syncthreads();
+        low = __reduce_min_sync(~0u, sm.warp_words[lane & (kWarps - 1)].high);
+        bound = (uint32_t)__syncthreads_count(shown >= low) >= want ? max(low, 1u) : 1u;
+        while (hi - bound >= 1u << 12) {
+            const uint32_t mid = hi - (hi - bound) / 2;
+            const uint32_t n = __syncthreads_count(shown >= mid);
+            if (n >= want) bound = mid;
+            else hi = mid - 1;
+            if (n >= want && n <= want + want / 8) break;
+        }
+    }
     Scale s;
     s.top = value_of(top_key);
     s.rate = greedy ? 1.f : fminf(__fdiv_rn(0x1.715476p+0f, temperature), 3e38f);
@@ -492,81 +526,77 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
             for (uint32_t i = tid; i < blocks * share; i += kThreads)
                 if (i % share < sm.counts[i / share]) sm.list[atomicAdd(&sm.n_list, 1u)] = sm.gather[i];
             __syncthreads();
+            // `team` threads a candidate, in no order: ranks and sums by comparison with every other
             const uint32_t n = sm.n_list;
-            constexpr int kOwn = kGather / kThreads;
-            uint64_t own[kOwn];
-#pragma unroll
-            for (int i = 0; i < kOwn; ++i) own[i] = tid + i * kThreads < (int)n ? sm.list[tid + i * kThreads] : 0;
-            // the first `want` of them: those not below the want-th
-            uint64_t last = 1;
-            if (n > want) {
-                uint64_t a = (uint64_t)bound << 32, b = (uint64_t)top_key << 32 | 0xffffffffu;
-                while (a < b) {
-                    const uint64_t mid = b - (b - a) / 2;
-                    int c = 0;
-#pragma unroll
-                    for (int i = 0; i < kOwn; ++i) c += own[i] >= mid;
-                    uint32_t total = __syncthreads_count(c > 0);
-#pragma unroll
-                    for (int i = 1; i < kOwn; ++i)
-                        if (n > (uint32_t)(i * kThreads)) total += __syncthreads_count(c > i);
-                    if (total >= want) a = mid;
-                    else b = mid - 1;
-                    if (total == want) b = a;
-                }
-                last = a;
-            }
+            for (uint32_t i = tid; i < n; i += kThreads) sm.weight[i] = weight_of(s, value_of((uint32_t)(sm.list[i] >> 32)));
+            int team_log2 = 0;
+            while (team_log2 < 5 && (n << (team_log2 + 1)) <= kThreads) ++team_log2;
+            const uint32_t team = 1u << team_log2, me0 = (uint32_t)tid >> team_log2, j0 = (uint32_t)tid & (team - 1);
+            constexpr int kRounds = kGather / kThreads;  // candidates of a thread, where they are many
+            uint64_t above[kRounds];
+            uint32_t rank_of[kRounds];
             __syncthreads();
-            if (tid == 0) sm.n_list = 0;
-            __syncthreads();
+            uint64_t total = 0;
 #pragma unroll
-            for (int i = 0; i < kOwn; ++i)
-                if (own[i] >= last) sm.list[atomicAdd(&sm.n_list, 1u)] = own[i];
-            __syncthreads();
-            // `team` threads a token, in no order: sums by comparison with every other token
-            const uint32_t m = sm.n_list;  // <= want
-            int team_log2 = 1;
-            while (team_log2 < 5 && (m << (team_log2 + 1)) <= kThreads) ++team_log2;
-            const uint32_t team = 1u << team_log2, i_me = (uint32_t)tid >> team_log2, j0 = (uint32_t)tid & (team - 1);
-            const uint64_t me = i_me < m ? sm.list[i_me] : 0;
-            const uint32_t index = ~(uint32_t)me;
-            uint32_t* ws = &sm.bins[0][0];
-            uint32_t w = i_me < m ? weight_of(s, value_of((uint32_t)(me >> 32))) : 0;
-            if (j0 == 0 && i_me < m) ws[i_me] = w;
-            __syncthreads();
-            uint64_t above = 0, sum = 0;
+            for (int q = 0; q < kRounds; ++q) {
+                const uint32_t i = me0 + q * kThreads;
+                above[q] = 0;
+                rank_of[q] = 0;
+                if (q > 0 && n <= (uint32_t)(q * kThreads)) break;
+                const uint64_t me = i < n ? sm.list[i] : ~0ull;
 #pragma unroll 4
-            for (uint32_t j = j0; j < m; j += team) {
-                const uint32_t wj = ws[j];
-                sum += wj;
-                above += sm.list[j] > me ? wj : 0u;
-            }
-            for (uint32_t off = 1; off < team; off <<= 1) {
-                sum += __shfl_xor_sync(~0u, sum, off);
-                above += __shfl_xor_sync(~0u, above, off);
-            }
-            const uint64_t goal = p_part < 0x80000000u ? share_of(k != 0xffffffffu ? sum : mass, p_part) : ~0ull;
-            // the nucleus ends among them, or they are all there is
-            const bool enough = k != 0xffffffffu || n < want || __syncthreads_or(i_me < m && above + w >= goal);
-            if (!(above < goal || above == 0) || w < least) w = 0;
-            __syncthreads();
-            if (j0 == 0 && i_me < m) ws[i_me] = w;
-            const uint32_t n_kept = __syncthreads_count(w > 0 && j0 == 0 && i_me < m);
-            if (enough) {
-                uint64_t before = 0;
-                sum = 0;
-#pragma unroll 4
-                for (uint32_t j = j0; j < m; j += team) {
-                    const uint32_t wj = ws[j];
-                    sum += wj;
-                    before += ~(uint32_t)sm.list[j] < index ? wj : 0u;
-                }
+                for (uint32_t j = j0; j < n; j += team)
+                    if (sm.list[j] > me) {
+                        above[q] += sm.weight[j];
+                        ++rank_of[q];
+                    }
                 for (uint32_t off = 1; off < team; off <<= 1) {
-                    sum += __shfl_xor_sync(~0u, sum, off);
-                    before += __shfl_xor_sync(~0u, before, off);
+                    above[q] += __shfl_xor_sync(~0u, above[q], off);
+                    rank_of[q] += __shfl_xor_sync(~0u, rank_of[q], off);
                 }
-                const uint64_t at_mass = share_of(sum, u_part);
-                if (j0 == 0 && i_me < m && w > 0 && before <= at_mass && at_mass < before + w) answer((int)index, w, sum, n_kept);
+                if (i < n && rank_of[q] < want) total = max(total, above[q] + sm.weight[i]);
+            }
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) total = max(total, __shfl_xor_sync(~0u, total, off));
+            if (lane == 0) sm.warp[wid].a = total;
+            __syncthreads();
+            for (int i = 0; i < kWarps; ++i) total = max(total, sm.warp[i].a);
+            // the nucleus ends among the first `want`, or they are all there is
+            const uint64_t goal = p_part < 0x80000000u ? share_of(k != 0xffffffffu ? total : mass, p_part) : ~0ull;
+            const bool enough = k != 0xffffffffu || n < want || total >= goal;
+            uint32_t n_kept = 0;
+#pragma unroll
+            for (int q = 0; q < kRounds; ++q) {
+                const uint32_t i = me0 + q * kThreads;
+                bool in = false;
+                if (i < n && j0 == 0) {
+                    const uint32_t w = sm.weight[i];
+                    in = rank_of[q] < want && (above[q] < goal || rank_of[q] == 0) && w >= least;
+                    sm.kept[i] = in ? w : 0u;
+                }
+                n_kept += __syncthreads_count(in);
+            }
+            if (enough) {
+#pragma unroll
+                for (int q = 0; q < kRounds; ++q) {
+                    const uint32_t i = me0 + q * kThreads;
+                    if (q > 0 && n <= (uint32_t)(q * kThreads)) break;
+                    const uint32_t index = i < n ? ~(uint32_t)sm.list[i] : 0u;
+                    uint64_t before = 0, sum = 0;
+#pragma unroll 4
+                    for (uint32_t j = j0; j < n; j += team) {
+                        const uint32_t wj = sm.kept[j];
+                        sum += wj;
+                        before += ~(uint32_t)sm.list[j] < index ? wj : 0u;
+                    }
+                    for (uint32_t off = 1; off < team; off <<= 1) {
+                        sum += __shfl_xor_sync(~0u, sum, off);
+                        before += __shfl_xor_sync(~0u, before, off);
+                    }
+                    const uint64_t at_mass = share_of(sum, u_part);
+                    const uint32_t w = i < n ? sm.kept[i] : 0u;
+                    if (j0 == 0 && before <= at_mass && at_mass < before + w) answer((int)index, w, sum, n_kept);
+                }
                 done = true;
             }
         }
