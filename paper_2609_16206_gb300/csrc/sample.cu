@@ -9,15 +9,17 @@
 // copies; everything after is passes over that copy and exchanges of a few
 // words over the cluster.  The kept tokens are the ones before a cut in the
 // order (falling logits, then index):
-//   * few of them (top-k up to kList, or a nucleus that is): every warp shows
-//     the largest of its lanes' maxima to the cluster, and the k-th largest of
-//     those is a bound that at least k logits reach and not many more do; those
-//     go to the first block, which ranks them;
+//   * top-k up to kList: every warp shows the largest of its lanes' maxima to
+//     the cluster, and the k-th largest of those is a bound that at least k
+//     logits reach and not many more do; those go to the first block, which
+//     ranks them;
 //   * a nucleus cut off by min-p anyway needs no cut: the mass of what min-p
 //     keeps, summed with the whole row's, shows it;
-//   * else the cut is found from the masses (or counts) of 512 bins of y, then
-//     of 512 parts of the bin that holds it, then by bisection over the part's
-//     keys, and over equal keys by index.
+//   * else the masses (or counts) of bins of y a unit wide, each thread's own,
+//     show the bin that holds the cut.  If few tokens stand up to its end they
+//     go to the first block as above; otherwise the bin's parts show the part,
+//     and the first block finds the cut in that (where the part is a crowd:
+//     bisection over its keys), or the index among equal keys.
 // Warps take contiguous runs of a block's part, so that the warps' sums say
 // where the drawn token lies, and only that run is gone through again.
 #include "decode_internal.cuh"
@@ -25,11 +27,12 @@
 namespace ctr {
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxCluster = 8;
 constexpr int kList = 256;          // tokens that the first block ranks
-constexpr int kGather = 1024;       // candidates of the cluster, an equal share of them to a block
-constexpr int kBins = 512;
+constexpr int kGather = 512;        // candidates of the cluster, an equal share of them to a block
+constexpr int kSpan = 24;           // bins of y, a unit each; what is lower goes to the last
+constexpr int kShared = 7;          // the first of them, of few tokens, are the block's; of the others each thread has its own,
+                                    // where its at most 255 weights below 2^24 have a sum below 2^32
 constexpr int kPieces = 4;          // of a block's part of the row, each a bulk copy
 constexpr uint32_t kEmptyKey = 0;   // of -inf and NaN
 constexpr unsigned kWaitLimit = 1u << 20;
@@ -154,25 +157,40 @@ __device__ __forceinline__ void remote_store32(uint32_t addr, uint32_t v)
 {
     asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(addr), "r"(v) : "memory");
 }
+__device__ __forceinline__ uint64_t remote_load64(uint32_t addr)
+{
+    uint64_t v;
+    asm volatile("ld.shared::cluster.u64 %0, [%1];" : "=l"(v) : "r"(addr) : "memory");
+    return v;
+}
 __device__ __forceinline__ uint32_t remote_load(uint32_t addr)
 {
     uint32_t v;
     asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(v) : "r"(addr) : "memory");
     return v;
 }
+// (the list is not made while bins are in use)
+template <int kThreads>
 struct __align__(16) Shared {
-    uint64_t gather[kGather];       // first block: (key, ~index) of the candidates
-    uint64_t list[kGather];         // the same without gaps
-    uint32_t weight[kGather];       // theirs
-    uint32_t kept[kGather];         // the same, 0 where not kept
-    uint32_t bins[3][kBins];        // low and high halves of the masses, counts
+    static constexpr int kWarps = kThreads / 32, kBins = kThreads;
+    union {
+        struct {
+            uint64_t gather[kGather];   // first block: (key, ~index) of the candidates
+            uint64_t list[kGather];     // the same without gaps
+            uint32_t weight[kGather];   // theirs
+            uint32_t kept[kGather];     // the same, 0 where not kept
+        };
+        uint32_t bins[2][kBins];        // low and high halves of the masses, or counts
+        uint32_t own_bins[kSpan - kShared][kThreads];
+    };
+    uint64_t unit_bins[kSpan];
     Sums warp[kWarps];
     Words warp_words[kWarps];
     Sums peers[2][kMaxCluster];     // exchanges alternate between the two
     Words peer_words[2][kMaxCluster];
     uint32_t shown[kThreads];       // the largest maxima of every warp of the cluster
     uint64_t warp_mass[kWarps];     // what each warp's run holds of the kept tokens
-    uint64_t found[3];
+    uint64_t found[2];
     uint32_t counts[kMaxCluster];   // candidates of each block
     uint32_t n_mine, n_list;
     uint64_t bar[kPieces];
@@ -230,11 +248,11 @@ template <> struct Vec<float> {
     static __device__ __forceinline__ float lowest() { return -INFINITY; }
 };
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams P)
+template <typename T, int kThreads>
+__global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const SampleParams P)
 {
-    constexpr int kN = Vec<T>::kN;
-    __shared__ Shared sm;
+    constexpr int kN = Vec<T>::kN, kWarps = kThreads / 32, kBins = kThreads;
+    __shared__ Shared<kThreads> sm;
     extern __shared__ __align__(16) unsigned char part_smem[];
     uint4* part = reinterpret_cast<uint4*>(part_smem);
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
@@ -309,7 +327,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         for (int j = 0; j < kN; ++j) most = fmaxf(most, e[j]);
     }
     uint32_t my_top = key_of(most);
-    const uint32_t want = k != 0xffffffffu ? k : (uint32_t)kList / 2;  // tokens that the bound has to let through
+    const uint32_t want = k != 0xffffffffu ? k : 1u;  // tokens that the bound has to let through
     // so many of each warp that the cluster's are a few times as many as wanted; a place for each of a block's threads
     const uint32_t places = kThreads / (kWarps * blocks);
     const uint32_t show = min(places, (3 * min(want, (uint32_t)kThreads) + kWarps * blocks - 1) / (kWarps * blocks));
@@ -428,7 +446,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
     // A key that at least `want` logits of the row reach: the want-th largest of the shown; 1 where not so many are.
     uint32_t bound = top_key;
-    if (k > 1 && !infinite) {
+    if (want > 1 && !infinite) {
         // from the warps' own maxima, if they are enough, to an eighth more than wanted or keys 2^12 near (2^-11 of a
         // logit)
         uint32_t low = __reduce_min_sync(~0u, tid % places == 0 ? shown : 0xffffffffu), hi = top_key;
@@ -463,55 +481,131 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         }
     };
 
-    // ---- without top-k: the row's mass, what min-p keeps of it, and what may stand before that in the order
-    bool cut = k != 0xffffffffu || p_part < 0x80000000u;
-    uint64_t mass = 0;
-    Sums kept = {0, 0, 0, 0}, kept_before = {0, 0, 0, 0};  // c: mass kept, n: tokens kept
-    if (k == 0xffffffffu) {
-        Sums v = {0, 0, 0, 0};
-        if (least == 1) {
-            each_pair([&](float, float, float y0, float y1, int) {
-                uint32_t w0, w1;
-                weights(s, y0, y1, w0, w1);
-                v.a += (uint64_t)w0 + w1;
-                v.n += min(w0, 1u) + min(w1, 1u);
-            });
-            v.c = v.a;
-        } else {
-            // Weights fall with the logits but for the rounding of the polynomial: `loose` is below every weight that
-            // can stand before one of `least` in the order.
-            const uint32_t loose = least - min(least, (least >> 20) + 1u);
-            each_pair([&](float, float, float y0, float y1, int) {
-                uint32_t w0, w1;
-                weights(s, y0, y1, w0, w1);
-                v.a += (uint64_t)w0 + w1;
-                if (max(w0, w1) < loose) return;
-                v.b += (uint64_t)(w0 >= loose ? w0 : 0u) + (w1 >= loose ? w1 : 0u);
-                v.c += (uint64_t)(w0 >= least ? w0 : 0u) + (w1 >= least ? w1 : 0u);
-                v.n += (w0 >= least) + (w1 >= least);
-            });
+    // ---- bins of y: masses (or counts) of units, then of a unit's kBins parts
+    auto unit_of = [](float y) { return min((int)-y, kSpan - 1); };
+    auto clear_units = [&] {
+#pragma unroll
+        for (int i = 0; i < kSpan - kShared; ++i) sm.own_bins[i][tid] = 0;
+        if (tid < kSpan) sm.unit_bins[tid] = 0;
+        __syncthreads();
+    };
+    auto add_to_unit = [&](int unit, uint32_t w) {
+        if (unit >= kShared) sm.own_bins[unit - kShared][tid] += w;
+        else atomicAdd(reinterpret_cast<unsigned long long*>(&sm.unit_bins[unit]), (unsigned long long)w);
+    };
+    // the block's units, then the cluster's: to every block, in peers' order
+    auto join_units = [&] {
+        __syncthreads();
+        for (int u = kShared + wid; u < kSpan; u += kWarps) {
+            uint64_t m = 0;
+            for (int i = lane; i < kThreads; i += 32) m += sm.own_bins[u - kShared][i];
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) m += __shfl_xor_sync(~0u, m, off);
+            if (lane == 0) sm.unit_bins[u] = m;
         }
-        kept = exchange(v, &kept_before);
-        if (lane == 0) sm.warp_mass[wid] = sm.warp[wid].c;
-        mass = kept.a;
-        // every token that min-p keeps comes before the nucleus ends
-        if (cut && least > 1 && kept.b <= share_of(mass, p_part)) cut = false;
-    }
+        if (blocks > 1) cluster_sync();
+        else __syncthreads();
+    };
+    // The first unit with which the sum over the cluster reaches the goal; `over` becomes the sum before it; -1: none
+    // does.
+    auto find_unit = [&](uint64_t goal, uint64_t& over) {
+        uint64_t m = 0;
+        if (lane < kSpan)
+            for (uint32_t b = 0; b < blocks; ++b) m += remote_load64(remote(smem_u32(&sm.unit_bins[lane]), b));
+        uint64_t upto = m;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const uint64_t a = __shfl_up_sync(~0u, upto, off);
+            if (lane >= off) upto += a;
+        }
+        const int unit = __ffs(__ballot_sync(~0u, upto >= goal)) - 1;
+        over = __shfl_sync(~0u, upto - m, max(unit, 0));
+        return unit;
+    };
+    auto part_index = [&](float y) { return (int)(-y * (float)kBins); };  // of all units' parts
+    // the same over the parts of a unit, on top of `over`; a barrier of the cluster stands before
+    auto find_part = [&](bool by_mass, uint64_t goal, uint64_t& over) {
+        uint64_t m = 0;  // of part `tid`
+        for (uint32_t b = 0; b < blocks; ++b) {
+            const uint32_t at = remote(smem_u32(&sm.bins[0][tid]), b);
+            m += remote_load(at);
+            if (by_mass) m += (uint64_t)remote_load(at + 4 * kBins) << 16;
+        }
+        uint64_t upto = m;
+#pragma unroll
+        for (int off = 1; off < 32; off <<= 1) {
+            const uint64_t a = __shfl_up_sync(~0u, upto, off);
+            if (lane >= off) upto += a;
+        }
+        if (lane == 31) sm.warp[wid].a = upto;
+        __syncthreads();
+        upto += over;
+        for (int i = 0; i < wid; ++i) upto += sm.warp[i].a;
+        if (upto >= goal && upto - m < goal) {
+            sm.found[0] = tid;
+            sm.found[1] = upto - m;
+        }
+        if (blocks > 1) cluster_sync();  // no block writes over its bins while another reads them
+        else __syncthreads();
+        over = sm.found[1];
+        return (int)sm.found[0];
+    };
 
-    // ---- few tokens: candidates to the first block
-    if (cut && want <= (uint32_t)kList) {
-        const uint32_t share = kGather / blocks, to = remote(smem_u32(sm.gather), 0) + 8 * rank * share;
-        for (uint32_t m = __ballot_sync(~0u, my_top >= bound); m; m &= m - 1) {  // the logits of a lane that reaches it
-            const int of = __ffs(m) - 1, n = (run1 - run0 - of + 31) / 32 * kN;
-            for (int i = lane; i < n; i += 32) {
-                const int at = (run0 + of + i / kN * 32) * kN + i % kN;
-                const uint32_t key = key_of(to_float(reinterpret_cast<const T*>(part)[at]));
-                if (key >= bound) {
-                    const uint32_t slot = atomicAdd(&sm.n_mine, 1u);
-                    if (slot < share) remote_store(to + 8 * slot, (uint64_t)key << 32 | (uint32_t)~(base + at));
-                }
+    // ---- the cut: keys above cut_key, and those equal to it up to cut_index
+    uint32_t cut_key = 1;
+    int cut_index = P.vocab;
+    auto in_cut = [&](uint32_t key, int i) { return key > cut_key || (key == cut_key && i <= cut_index); };
+    // A unit's parts, of the tokens of the cut with keys >= floor: into sm.bins; the words are the unit's smallest key
+    // (complemented) and the number of tokens in it and above it.
+    auto split_unit = [&](bool by_mass, int unit, uint32_t floor) {
+        for (int i = tid; i < 2 * kBins; i += kThreads) (&sm.bins[0][0])[i] = 0;
+        __syncthreads();
+        const int from = unit * kBins;
+        const bool open = unit == kSpan - 1;  // to below
+        Words v = {0, 0, 0};
+        each_pair([&](float x0, float x1, float y0, float y1, int at) {
+            const float y[2] = {y0, y1}, e[2] = {x0, x1};
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                const int b = part_index(y[j]) - from;
+                if (b >= kBins && !open) continue;
+                const uint32_t key = key_of(e[j]);
+                if (key < floor || !in_cut(key, at + j)) continue;
+                ++v.n;
+                if (b < 0) continue;
+                v.high = max(v.high, ~key);
+                const uint32_t w = by_mass ? weight_of(s, e[j]) : 1u;
+                atomicAdd(&sm.bins[0][min(b, kBins - 1)], w & 0xffffu);
+                if (by_mass) atomicAdd(&sm.bins[1][min(b, kBins - 1)], w >> 16);
             }
-            __syncwarp();
+        });
+        return exchange_words(v);
+    };
+    // The first block's list of the tokens of the cut with keys in [low, high], from threads whose own maximum reaches
+    // `low`; false where there is no room for them (which every block knows).
+    auto gather = [&](uint32_t low, uint32_t high, bool few_threads) {
+        const uint32_t share = kGather / blocks, to = remote(smem_u32(sm.gather), 0) + 8 * rank * share;
+        auto put = [&](uint32_t key, int at) {
+            if (key < low || key > high || !in_cut(key, at)) return;
+            const uint32_t slot = atomicAdd(&sm.n_mine, 1u);
+            if (slot < share) remote_store(to + 8 * slot, (uint64_t)key << 32 | (uint32_t)~at);
+        };
+        if (few_threads) {
+            for (uint32_t m = __ballot_sync(~0u, my_top >= low); m; m &= m - 1) {  // the warp on one thread's logits
+                const int of = __ffs(m) - 1, n = (run1 - run0 - of + 31) / 32 * kN;
+                for (int i = lane; i < n; i += 32) {
+                    const int at = (run0 + of + i / kN * 32) * kN + i % kN;
+                    put(key_of(to_float(reinterpret_cast<const T*>(part)[at])), base + at);
+                }
+                __syncwarp();
+            }
+        } else {
+            for (int v = run0 + lane; v < run1; v += 32) {
+                float e[kN];
+                Vec<T>::split(part[v], e);
+#pragma unroll
+                for (int j = 0; j < kN; ++j) put(key_of(e[j]), base + v * kN + j);
+            }
         }
         __syncthreads();
         if (tid < (int)blocks) remote_store32(remote(smem_u32(&sm.counts[rank]), tid), sm.n_mine);
@@ -520,222 +614,95 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         else __syncthreads();
         bool fits = true;
         for (uint32_t i = 0; i < blocks; ++i) fits = fits && sm.counts[i] <= share;
-        if (fits && k != 0xffffffffu && rank != 0) return;
-        bool done = false;  // the first block has the token
-        if (fits && rank == 0) {
+        if (tid == 0) sm.n_mine = 0;
+        if (rank == 0 && fits) {
             for (uint32_t i = tid; i < blocks * share; i += kThreads)
                 if (i % share < sm.counts[i / share]) sm.list[atomicAdd(&sm.n_list, 1u)] = sm.gather[i];
-            __syncthreads();
-            // `team` threads a candidate, in no order: ranks and sums by comparison with every other
-            const uint32_t n = sm.n_list;
-            for (uint32_t i = tid; i < n; i += kThreads) sm.weight[i] = weight_of(s, value_of((uint32_t)(sm.list[i] >> 32)));
-            int team_log2 = 0;
-            while (team_log2 < 5 && (n << (team_log2 + 1)) <= kThreads) ++team_log2;
-            const uint32_t team = 1u << team_log2, me0 = (uint32_t)tid >> team_log2, j0 = (uint32_t)tid & (team - 1);
-            constexpr int kRounds = kGather / kThreads;  // candidates of a thread, where they are many
-            uint64_t above[kRounds];
-            uint32_t rank_of[kRounds];
-            __syncthreads();
-            uint64_t total = 0;
-#pragma unroll
-            for (int q = 0; q < kRounds; ++q) {
-                const uint32_t i = me0 + q * kThreads;
-                above[q] = 0;
-                rank_of[q] = 0;
-                if (q > 0 && n <= (uint32_t)(q * kThreads)) break;
-                const uint64_t me = i < n ? sm.list[i] : ~0ull;
-#pragma unroll 4
-                for (uint32_t j = j0; j < n; j += team)
-                    if (sm.list[j] > me) {
-                        above[q] += sm.weight[j];
-                        ++rank_of[q];
-                    }
-                for (uint32_t off = 1; off < team; off <<= 1) {
-                    above[q] += __shfl_xor_sync(~0u, above[q], off);
-                    rank_of[q] += __shfl_xor_sync(~0u, rank_of[q], off);
-                }
-                if (i < n && rank_of[q] < want) total = max(total, above[q] + sm.weight[i]);
-            }
-#pragma unroll
-            for (int off = 16; off > 0; off >>= 1) total = max(total, __shfl_xor_sync(~0u, total, off));
-            if (lane == 0) sm.warp[wid].a = total;
-            __syncthreads();
-            for (int i = 0; i < kWarps; ++i) total = max(total, sm.warp[i].a);
-            // the nucleus ends among the first `want`, or they are all there is
-            const uint64_t goal = p_part < 0x80000000u ? share_of(k != 0xffffffffu ? total : mass, p_part) : ~0ull;
-            const bool enough = k != 0xffffffffu || n < want || total >= goal;
-            uint32_t n_kept = 0;
-#pragma unroll
-            for (int q = 0; q < kRounds; ++q) {
-                const uint32_t i = me0 + q * kThreads;
-                bool in = false;
-                if (i < n && j0 == 0) {
-                    const uint32_t w = sm.weight[i];
-                    in = rank_of[q] < want && (above[q] < goal || rank_of[q] == 0) && w >= least;
-                    sm.kept[i] = in ? w : 0u;
-                }
-                n_kept += __syncthreads_count(in);
-            }
-            if (enough) {
-#pragma unroll
-                for (int q = 0; q < kRounds; ++q) {
-                    const uint32_t i = me0 + q * kThreads;
-                    if (q > 0 && n <= (uint32_t)(q * kThreads)) break;
-                    const uint32_t index = i < n ? ~(uint32_t)sm.list[i] : 0u;
-                    uint64_t before = 0, sum = 0;
-#pragma unroll 4
-                    for (uint32_t j = j0; j < n; j += team) {
-                        const uint32_t wj = sm.kept[j];
-                        sum += wj;
-                        before += ~(uint32_t)sm.list[j] < index ? wj : 0u;
-                    }
-                    for (uint32_t off = 1; off < team; off <<= 1) {
-                        sum += __shfl_xor_sync(~0u, sum, off);
-                        before += __shfl_xor_sync(~0u, before, off);
-                    }
-                    const uint64_t at_mass = share_of(sum, u_part);
-                    const uint32_t w = i < n ? sm.kept[i] : 0u;
-                    if (j0 == 0 && before <= at_mass && at_mass < before + w) answer((int)index, w, sum, n_kept);
-                }
-                done = true;
-            }
         }
-        if (fits && (k != 0xffffffffu || exchange_words(Words{done ? 1u : 0u, 0, 0}).top)) return;
-    }
-
-    // ---- the cut: keys above cut_key, and those equal to it up to cut_index
-    uint32_t cut_key = 1;
-    int cut_index = P.vocab;
-    auto in_cut = [&](uint32_t key, int i) { return key > cut_key || (key == cut_key && i <= cut_index); };
-    // moves the cut to the first tokens of the order that reach `n_goal` tokens or the mass `goal`, all of whose keys
-    // are at least `floor`
-    auto cut_at = [&](uint32_t n_goal, uint64_t goal, uint32_t floor) {
-        uint64_t over = 0;      // mass and count above the part of a bin that the cut lies in
-        uint32_t n_over = 0;
-        int from = 0;           // the part, in units of the level
-        for (int level = 0; level < 2; ++level) {
-            const float unit = level == 0 ? 16.f : 16.f * kBins;  // bins of y a unit
-            for (int i = tid; i < 3 * kBins; i += kThreads) (&sm.bins[0][0])[i] = 0;
-            __syncthreads();
-            each_pair([&](float x0, float x1, float y0, float y1, int at) {
-                const float y[2] = {y0, y1}, e[2] = {x0, x1};
-                uint32_t w[2];
-                int bin[2];
-                bool in[2];
+        __syncthreads();
+        return fits;
+    };
+    // The first block, on its list: `team` threads a candidate, in no order, compare it with every other.  f(which of
+    // this thread's candidates, its number, those above it, their weight) on a team's first thread.
+    constexpr int kRounds = kGather / kThreads;  // candidates of a thread, where they are many
+    auto rank_list = [&](uint32_t n, auto&& weight, auto&& f) {
+        for (uint32_t i = tid; i < n; i += kThreads) sm.weight[i] = weight((uint32_t)(sm.list[i] >> 32));
+        int team_log2 = 0;
+        while (team_log2 < 5 && (n << (team_log2 + 1)) <= kThreads) ++team_log2;
+        const uint32_t team = 1u << team_log2, me0 = (uint32_t)tid >> team_log2, j0 = (uint32_t)tid & (team - 1);
+        __syncthreads();
 #pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    bin[j] = (int)(-y[j] * unit) - from;
-                    const uint32_t key = key_of(e[j]);
-                    in[j] = key >= floor && in_cut(key, at + j) && bin[j] >= 0 && (level == 0 || bin[j] < kBins || from == (kBins - 1) * kBins);
-                    bin[j] = min(bin[j], kBins - 1);
+        for (int q = 0; q < kRounds; ++q) {
+            const uint32_t i = me0 + q * kThreads;
+            const uint64_t me = i < n ? sm.list[i] : ~0ull;
+            uint64_t above = 0;
+            uint32_t before = 0;
+            if (q > 0 && n <= (uint32_t)(q * kThreads)) break;
+#pragma unroll 4
+            for (uint32_t j = j0; j < n; j += team)
+                if (sm.list[j] > me) {
+                    above += sm.weight[j];
+                    ++before;
                 }
-                if (!in[0] && !in[1]) return;
-                weights(s, y0, y1, w[0], w[1]);
-#pragma unroll
-                for (int j = 0; j < 2; ++j)
-                    if (in[j]) {
-                        atomicAdd(&sm.bins[0][bin[j]], w[j] & 0xffffu);
-                        atomicAdd(&sm.bins[1][bin[j]], w[j] >> 16);
-                        atomicAdd(&sm.bins[2][bin[j]], 1u);
-                    }
-            });
-            if (blocks > 1) cluster_sync();
-            else __syncthreads();
-            // a bin a thread: its sums over the cluster, then over the bins before it
-            uint64_t m = 0;
-            uint32_t c = 0;
-            for (uint32_t b = 0; b < blocks; ++b) {
-                const uint32_t at = remote(smem_u32(&sm.bins[0][tid]), b);
-                m += (uint64_t)remote_load(at) + ((uint64_t)remote_load(at + 4 * kBins) << 16);
-                c += remote_load(at + 8 * kBins);
+            for (uint32_t off = 1; off < team; off <<= 1) {
+                above += __shfl_xor_sync(~0u, above, off);
+                before += __shfl_xor_sync(~0u, before, off);
             }
-            uint64_t ms = m;
-            uint32_t cs = c;
-#pragma unroll
-            for (int off = 1; off < 32; off <<= 1) {
-                const uint64_t a = __shfl_up_sync(~0u, ms, off);
-                const uint32_t b = __shfl_up_sync(~0u, cs, off);
-                if (lane >= off) ms += a, cs += b;
-            }
-            if (lane == 31) {
-                sm.warp[wid].a = ms;
-                sm.warp[wid].n = cs;
-            }
-            if (tid == 0) sm.found[0] = ~0ull;
-            __syncthreads();
-            ms += over;
-            cs += n_over;
-            for (int i = 0; i < wid; ++i) ms += sm.warp[i].a, cs += sm.warp[i].n;
-            const bool at_goal = cs >= n_goal || ms >= goal, before = cs - c >= n_goal || ms - m >= goal;
-            if (at_goal && !before) {
-                sm.found[0] = tid;
-                sm.found[1] = ms - m;
-                sm.found[2] = cs - c;
-            }
-            if (blocks > 1) cluster_sync();  // no block clears its bins while another reads them
-            else __syncthreads();
-            if (sm.found[0] == ~0ull) return;  // the goal is beyond all of them
-            over = sm.found[1];
-            n_over = (uint32_t)sm.found[2];
-            from = level == 0 ? (int)sm.found[0] * kBins : from + (int)sm.found[0];
-            __syncthreads();
+            if (i < n && j0 == 0) f(q, i, before, above);
         }
-        const bool last_bin = from == kBins * kBins - 1;  // open to below
-        auto in_part = [&](float y) {
-            const int b = (int)(-y * (16.f * kBins));
-            return last_bin ? b >= from : b == from;
-        };
-        // the part's largest and smallest key
-        uint32_t low = 0xffffffffu, high = 0;
+    };
+    // The cut goes to the first tokens of the order whose mass (or number) reaches the goal: it lies in `unit`, above
+    // which stands `over`, and whose parts are in sm.bins.
+    auto cut_in = [&](bool by_mass, uint64_t goal, uint64_t over, int unit, uint32_t floor) {
+        const int from = unit * kBins + find_part(by_mass, goal, over);
+        const bool open = from == kSpan * kBins - 1;
+        // the part's largest and smallest key: in between are its tokens alone
+        Words v = {0, 0, 0};
         each_pair([&](float x0, float x1, float y0, float y1, int at) {
-            const float y[2] = {y0, y1}, e[2] = {x0, x1};
-#pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                if (!in_part(y[j])) continue;
-                const uint32_t key = key_of(e[j]);
-                if (key >= floor && in_cut(key, at + j)) {
-                    low = min(low, key);
-                    high = max(high, key);
-                }
-            }
+            const int b0 = part_index(y0), b1 = part_index(y1);
+            if (max(b0, b1) < from || (min(b0, b1) > from && !open)) return;
+            const uint32_t k0 = key_of(x0), k1 = key_of(x1);
+            if ((b0 == from || (open && b0 > from)) && k0 >= floor && in_cut(k0, at)) v = Words{max(v.top, k0), max(v.high, ~k0), v.n + 1};
+            if ((b1 == from || (open && b1 > from)) && k1 >= floor && in_cut(k1, at + 1)) v = Words{max(v.top, k1), max(v.high, ~k1), v.n + 1};
         });
-        const Words ends = exchange_words(Words{high, ~low, 0});
-        uint32_t hi_key = ends.top, lo_key = ~ends.high;
-        Sums v = {0, 0, 0, 0};
+        v = exchange_words(v);
+        uint32_t hi_key = v.top, lo_key = ~v.high;
+        auto weight = [&](uint32_t key) { return by_mass ? weight_of(s, value_of(key)) : 1u; };
+        if (lo_key < hi_key && gather(lo_key, hi_key, false)) {
+            Words c = {0, 0, 0};  // the token that reaches the goal
+            if (rank == 0) {
+                const uint32_t n = sm.n_list;
+                rank_list(n, weight, [&](int, uint32_t i, uint32_t, uint64_t above) {
+                    if (over + above < goal && goal <= over + above + sm.weight[i]) c = Words{(uint32_t)(sm.list[i] >> 32), ~(uint32_t)sm.list[i] + 1u, 0};
+                });
+            }
+            c = exchange_words(c);
+            if (tid == 0) sm.n_list = 0;
+            cut_key = c.top;
+            cut_index = (int)c.high - 1;
+            return;
+        }
+        uint64_t above = 0;  // of the part, before the cut's key
         auto tally_part = [&](uint32_t from_key) {  // the part's keys >= from_key
             Sums t = {0, 0, 0, 0};
-            each_pair([&](float x0, float x1, float y0, float y1, int at) {
-                const float y[2] = {y0, y1}, e[2] = {x0, x1};
-                if (!in_part(y0) && !in_part(y1)) return;
-                uint32_t w[2];
-                weights(s, y0, y1, w[0], w[1]);
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    const uint32_t key = key_of(e[j]);
-                    if (key >= from_key && key >= floor && in_part(y[j]) && in_cut(key, at + j)) {
-                        t.a += w[j];
-                        t.n += 1;
-                    }
-                }
+            each_pair([&](float x0, float x1, float, float, int at) {
+                const uint32_t k0 = key_of(x0), k1 = key_of(x1);
+                if (k0 >= from_key && k0 <= v.top && in_cut(k0, at)) t.a += weight(k0);
+                if (k1 >= from_key && k1 <= v.top && in_cut(k1, at + 1)) t.a += weight(k1);
             });
-            return exchange(t, nullptr);
+            return exchange(t, nullptr).a;
         };
         if (lo_key < hi_key) {
             while (lo_key < hi_key) {
                 const uint32_t mid = hi_key - (hi_key - lo_key) / 2;
-                v = tally_part(mid);
-                if (n_over + v.n >= n_goal || over + v.a >= goal) lo_key = mid;
+                if (over + tally_part(mid) >= goal) lo_key = mid;
                 else hi_key = mid - 1;
             }
-            v = tally_part(lo_key + 1);
+            if (lo_key < v.top) above = tally_part(lo_key + 1);
         }
         // of the tokens equal to it, those still needed, by index
-        const uint32_t w = weight_of(s, value_of(lo_key));
-        uint64_t need = n_goal - n_over - v.n;
-        if (goal != ~0ull) {
-            const uint64_t by_mass = w > 0 ? (goal - over - v.a + w - 1) / w : ~0ull;
-            need = by_mass < need ? by_mass : need;
-        }
+        const uint32_t each = weight(lo_key);
+        const uint64_t need = (goal - over - above + each - 1) / each;
         uint32_t c = 0;
         each_pair([&](float x0, float x1, float, float, int at) {
             c += (key_of(x0) == lo_key && in_cut(lo_key, at)) + (key_of(x1) == lo_key && in_cut(lo_key, at + 1));
@@ -762,22 +729,171 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
         cut_index = (int)exchange_words(Words{index, 0, 0}).top - 1;  // the goal is reached, so that there is one
         cut_key = lo_key;
     };
-    if (cut) {
-        if (k != 0xffffffffu) cut_at(k, ~0ull, bound);
-        if (p_part < 0x80000000u) {
-            if (k != 0xffffffffu) {
-                Sums v = {0, 0, 0, 0};
-                each_pair([&](float x0, float x1, float y0, float y1, int at) {
-                    const bool in0 = in_cut(key_of(x0), at), in1 = in_cut(key_of(x1), at + 1);
-                    if (!in0 && !in1) return;
+    // the cut to the first tokens that reach the goal, among those with keys >= floor; nothing where they do not
+    auto cut_at = [&](bool by_mass, uint64_t goal, uint32_t floor) {
+        clear_units();
+        each_pair([&](float x0, float x1, float y0, float y1, int at) {
+            const bool in0 = key_of(x0) >= floor && in_cut(key_of(x0), at), in1 = key_of(x1) >= floor && in_cut(key_of(x1), at + 1);
+            if (!in0 && !in1) return;
+            uint32_t w0 = 1, w1 = 1;
+            if (by_mass) weights(s, y0, y1, w0, w1);
+            if (in0) add_to_unit(unit_of(y0), w0);
+            if (in1) add_to_unit(unit_of(y1), w1);
+        });
+        join_units();
+        uint64_t over = 0;
+        const int unit = find_unit(goal, over);
+        if (blocks > 1) cluster_sync();
+        else __syncthreads();
+        if (unit < 0) return;
+        split_unit(by_mass, unit, floor);
+        cut_in(by_mass, goal, over, unit, floor);
+    };
+
+    // ---- without top-k: the row's mass, what min-p keeps of it, and what may stand before that in the order
+    bool cut = k != 0xffffffffu || p_part < 0x80000000u;
+    bool by_list = k <= (uint32_t)kList;
+    Sums kept = {0, 0, 0, 0}, kept_before = {0, 0, 0, 0};  // c: mass kept, n: tokens kept
+    uint64_t goal = ~0ull, over = 0;                       // of the nucleus; the mass above its last unit
+    int unit = -1;
+    if (k == 0xffffffffu) {
+        Sums v = {0, 0, 0, 0};
+        // Weights fall with the logits but for the rounding of the polynomial: `loose` is below every weight that can
+        // stand before one of `least` in the order.
+        const uint32_t loose = least == 1 ? 0 : least - min(least, (least >> 20) + 1u);
+        if (least > 1) {
+            each_pair([&](float, float, float y0, float y1, int) {
+                uint32_t w0, w1;
+                weights(s, y0, y1, w0, w1);
+                v.a += (uint64_t)w0 + w1;
+                if (max(w0, w1) < loose) return;
+                v.b += (uint64_t)(w0 >= loose ? w0 : 0u) + (w1 >= loose ? w1 : 0u);
+                v.c += (uint64_t)(w0 >= least ? w0 : 0u) + (w1 >= least ? w1 : 0u);
+                v.n += (w0 >= least) + (w1 >= least);
+            });
+        } else if (cut) {
+            clear_units();
+            each_pair([&](float, float, float y0, float y1, int) {
+                uint32_t w0, w1;
+                weights(s, y0, y1, w0, w1);
+                v.a += (uint64_t)w0 + w1;
+                add_to_unit(unit_of(y0), w0);
+                add_to_unit(unit_of(y1), w1);
+            });
+        } else {
+            each_pair([&](float, float, float y0, float y1, int) {
+                uint32_t w0, w1;
+                weights(s, y0, y1, w0, w1);
+                v.c += (uint64_t)w0 + w1;
+                v.n += min(w0, 1u) + min(w1, 1u);
+            });
+        }
+        kept = exchange(v, &kept_before);
+        if (lane == 0) sm.warp_mass[wid] = sm.warp[wid].c;
+        if (cut) {
+            goal = max(share_of(kept.a, p_part), (uint64_t)1);
+            // every token that min-p keeps comes before the nucleus ends
+            if (least > 1 && kept.b <= goal) cut = false;
+        }
+        if (cut) {
+            if (least > 1) {  // the nucleus ends above what min-p leaves out: no lower unit than `loose` falls in, or the next
+                clear_units();
+                const int last = unit_of(log2f((float)max(loose, 1u)) - 31.f) + 1;
+                each_pair([&](float, float, float y0, float y1, int) {
+                    const int u0 = unit_of(y0), u1 = unit_of(y1);
+                    if (min(u0, u1) > last) return;
                     uint32_t w0, w1;
                     weights(s, y0, y1, w0, w1);
-                    v.a += (uint64_t)(in0 ? w0 : 0u) + (in1 ? w1 : 0u);
+                    if (u0 <= last) add_to_unit(u0, w0);
+                    if (u1 <= last) add_to_unit(u1, w1);
                 });
-                mass = exchange(v, nullptr).a;
             }
-            const uint64_t goal = share_of(mass, p_part);
-            cut_at(0xffffffffu, goal > 0 ? goal : 1, cut_key);
+            join_units();
+            unit = find_unit(goal, over);
+            if (blocks > 1) cluster_sync();  // no block goes on to other bins while another reads these
+            else __syncthreads();
+            const Words in = split_unit(true, unit, 1);
+            // few tokens up to the unit's end: no block has more than its share of the list
+            by_list = in.n <= (uint32_t)min(kList, (int)(kGather / blocks));
+            bound = ~in.high;
+        }
+    }
+
+    // ---- few tokens: the first block has them all
+    if (cut && by_list && gather(bound, 0xffffffffu, true)) {
+        if (rank != 0) return;
+        const uint32_t n = sm.n_list;
+        uint64_t above[kRounds], total = 0;
+        uint32_t place[kRounds], number[kRounds];
+#pragma unroll
+        for (int q = 0; q < kRounds; ++q) number[q] = kGather;
+        rank_list(n, [&](uint32_t key) { return weight_of(s, value_of(key)); },
+                  [&](int q, uint32_t i, uint32_t before, uint64_t a) {
+                      above[q] = a;
+                      place[q] = before;
+                      number[q] = i;
+                      if (before < k) total = max(total, a + sm.weight[i]);
+                  });
+        if (k != 0xffffffffu && p_part < 0x80000000u) {  // of the top-k's mass
+#pragma unroll
+            for (int off = 16; off > 0; off >>= 1) total = max(total, __shfl_xor_sync(~0u, total, off));
+            if (lane == 0) sm.warp[wid].a = total;
+            __syncthreads();
+            for (int i = 0; i < kWarps; ++i) total = max(total, sm.warp[i].a);
+            goal = share_of(total, p_part);
+        }
+        // the kept ones, and where each stands among them in the vocabulary
+        uint32_t n_kept = 0;
+#pragma unroll
+        for (int q = 0; q < kRounds; ++q) {
+            bool in = false;
+            if (number[q] < n) {
+                const uint32_t w = sm.weight[number[q]];
+                in = place[q] < k && (above[q] < goal || place[q] == 0) && w >= least;
+                sm.kept[number[q]] = in ? w : 0u;
+            }
+            n_kept += __syncthreads_count(in);
+        }
+        int team_log2 = 0;
+        while (team_log2 < 5 && (n << (team_log2 + 1)) <= kThreads) ++team_log2;
+        const uint32_t team = 1u << team_log2, me0 = (uint32_t)tid >> team_log2, j0 = (uint32_t)tid & (team - 1);
+#pragma unroll
+        for (int q = 0; q < kRounds; ++q) {
+            const uint32_t i = me0 + q * kThreads;
+            if (q > 0 && n <= (uint32_t)(q * kThreads)) break;
+            const uint32_t index = i < n ? ~(uint32_t)sm.list[i] : 0u;
+            uint64_t before = 0, sum = 0;
+#pragma unroll 4
+            for (uint32_t j = j0; j < n; j += team) {
+                const uint32_t wj = sm.kept[j];
+                sum += wj;
+                before += ~(uint32_t)sm.list[j] < index ? wj : 0u;
+            }
+            for (uint32_t off = 1; off < team; off <<= 1) {
+                sum += __shfl_xor_sync(~0u, sum, off);
+                before += __shfl_xor_sync(~0u, before, off);
+            }
+            const uint64_t at_mass = share_of(sum, u_part);
+            const uint32_t w = i < n ? sm.kept[i] : 0u;
+            if (j0 == 0 && before <= at_mass && at_mass < before + w) answer((int)index, w, sum, n_kept);
+        }
+        return;
+    }
+
+    // ---- many: the cut, and what stands before it
+    if (cut) {
+        if (k != 0xffffffffu) {
+            cut_at(false, k, bound);
+            if (p_part < 0x80000000u) {
+                Sums v = {0, 0, 0, 0};
+                each_pair([&](float x0, float x1, float, float, int at) {
+                    v.a += (uint64_t)(in_cut(key_of(x0), at) ? weight_of(s, x0) : 0u) + (in_cut(key_of(x1), at + 1) ? weight_of(s, x1) : 0u);
+                });
+                goal = max(share_of(exchange(v, nullptr).a, p_part), (uint64_t)1);
+                cut_at(true, goal, cut_key);
+            }
+        } else {
+            cut_in(true, goal, over, unit, 1);
         }
         Sums v = {0, 0, 0, 0};
         each_pair([&](float x0, float x1, float y0, float y1, int at) {
@@ -795,7 +911,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
 
     // ---- the draw: the warp's run that holds it, shared out over the block
-    const uint64_t goal = share_of(kept.c, u_part);
+    goal = share_of(kept.c, u_part);
     __syncthreads();
     uint64_t run_begin = kept_before.c;
     int run = 0;
@@ -834,20 +950,28 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleParams 
     }
 }
 
+template <typename T, int kThreads>
+cudaError_t launch_as(const SampleParams& p, int blocks, size_t bytes, cudaStream_t stream)
+{
+    auto kernel = sample_kernel<T, kThreads>;
+    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    if (err != cudaSuccess) return err;
+    return launch_dependent(kernel, dim3((unsigned)(p.n_rows * blocks)), dim3(kThreads), bytes, blocks, stream, p);
+}
+
 template <typename T>
 cudaError_t launch_typed(const SampleParams& p, cudaStream_t stream)
 {
     constexpr int kN = Vec<T>::kN;
     const int n_vec = (p.vocab + 2 * kN - 2) / kN;  // at the worst alignment
-    // as many blocks a row as keep the GPU's two an SM busy, and as its shared memory needs
+    // Blocks a row: parts of at most 40 KB, so that four blocks share an SM and one's waits hide behind the others'
+    // work; more where the rows are few, down to parts of a kilobyte.
     int blocks = 1;
-    while (blocks < kMaxCluster && ((int64_t)p.n_rows * blocks < 304 || (n_vec + blocks - 1) / blocks * 16 > 72 * 1024)) blocks *= 2;
+    while (blocks < kMaxCluster && ((int64_t)p.n_rows * blocks < 304 || (n_vec + blocks - 1) / blocks * 16 > 40 * 1024)) blocks *= 2;
     while (blocks > 1 && n_vec / blocks < 64) blocks /= 2;
     const size_t bytes = (size_t)(n_vec + blocks - 1) / blocks * 16;
-    auto kernel = sample_kernel<T>;
-    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-    if (err != cudaSuccess) return err;
-    return launch_dependent(kernel, dim3((unsigned)(p.n_rows * blocks)), dim3(kThreads), bytes, blocks, stream, p);
+    // where a block has an SM to itself, twice the threads
+    return (int64_t)p.n_rows * blocks <= 152 ? launch_as<T, 512>(p, blocks, bytes, stream) : launch_as<T, 256>(p, blocks, bytes, stream);
 }
 
 }  // namespace
