@@ -30,7 +30,7 @@ namespace {
 constexpr int kMaxCluster = 8;
 constexpr int kList = 256;          // tokens that the first block ranks
 constexpr int kGather = 512;        // candidates of the cluster, an equal share of them to a block
-constexpr int kSpan = 24;           // bins of y, a unit each; what is lower goes to the last
+constexpr int kUnits = 25;          // bins of y: (-1, 0] .. (-16, -15], then twos to -34, below which no weight is left
 constexpr int kShared = 7;          // the first of them, of few tokens, are the block's; of the others each thread has its own,
                                     // where its at most 255 weights below 2^24 have a sum below 2^32
 constexpr int kPieces = 4;          // of a block's part of the row, each a bulk copy
@@ -80,22 +80,23 @@ __device__ __forceinline__ void exponents(const Scale& s, float x0, float x1, fl
     y1 = fmaxf(__uint_as_float((uint32_t)(y >> 32)), -64.f);
 }
 
-// round(2^31 2^y): y = k + f with k its nearest integer (by adding 1.5 2^23, whose low bits are then k), 2^f =
+// round(2^31 2^y): y = k + f with k its nearest integer (by adding 1.5 2^23 + 32, whose low bits are then k + 32), 2^f =
 // 1 + f (c1 + f (c2 + ...)), a minimax fit on [-1/2, 1/2] with constant term 1: relative error 9.2e-8 before
-// rounding and 1.9e-7 with every fp32 step rounded.
+// rounding and 1.9e-7 with every fp32 step rounded.  Half of it is computed, which rounds alike.
 __device__ __forceinline__ void weights(const Scale& s, float y0, float y1, uint32_t& w0, uint32_t& w1)
 {
-    const uint64_t y = pack(y0, y1), magic = pack(0x1.8p+23f, 0x1.8p+23f);
-    const uint64_t t = add2(y, magic), k = add2(t, pack(-0x1.8p+23f, -0x1.8p+23f));
+    constexpr float kMagic = 0x1.8p+23f + 32.f;
+    const uint64_t y = pack(y0, y1);
+    const uint64_t t = add2(y, pack(kMagic, kMagic)), k = add2(t, pack(-kMagic, -kMagic));
     const uint64_t f = fma2(k, pack(-1.f, -1.f), y);
-    uint64_t p = pack(0x1.5bba14p-10f, 0x1.5bba14p-10f);
-    p = add2(fma2(p, f, s.mz), pack(0x1.3cea88p-7f, 0x1.3cea88p-7f));
-    p = add2(fma2(p, f, s.mz), pack(0x1.c6b752p-5f, 0x1.c6b752p-5f));
-    p = add2(fma2(p, f, s.mz), pack(0x1.ebf9bcp-3f, 0x1.ebf9bcp-3f));
-    p = add2(fma2(p, f, s.mz), pack(0x1.62e42ap-1f, 0x1.62e42ap-1f));
-    p = add2(fma2(p, f, s.mz), pack(1.f, 1.f));
-    w0 = __float2uint_rn(__uint_as_float((uint32_t)p + ((uint32_t)t << 23) + (31u << 23)));
-    w1 = __float2uint_rn(__uint_as_float((uint32_t)(p >> 32) + ((uint32_t)(t >> 32) << 23) + (31u << 23)));
+    uint64_t p = pack(0x1.5bba14p-11f, 0x1.5bba14p-11f);
+    p = add2(fma2(p, f, s.mz), pack(0x1.3cea88p-8f, 0x1.3cea88p-8f));
+    p = add2(fma2(p, f, s.mz), pack(0x1.c6b752p-6f, 0x1.c6b752p-6f));
+    p = add2(fma2(p, f, s.mz), pack(0x1.ebf9bcp-4f, 0x1.ebf9bcp-4f));
+    p = add2(fma2(p, f, s.mz), pack(0x1.62e42ap-2f, 0x1.62e42ap-2f));
+    p = add2(fma2(p, f, s.mz), pack(0.5f, 0.5f));
+    w0 = __float2uint_rn(__uint_as_float((uint32_t)p + ((uint32_t)t << 23)));
+    w1 = __float2uint_rn(__uint_as_float((uint32_t)(p >> 32) + ((uint32_t)(t >> 32) << 23)));
 }
 __device__ __forceinline__ uint32_t weight_of(const Scale& s, float x)
 {
@@ -181,9 +182,9 @@ struct __align__(16) Shared {
             uint32_t kept[kGather];     // the same, 0 where not kept
         };
         uint32_t bins[2][kBins];        // low and high halves of the masses, or counts
-        uint32_t own_bins[kSpan - kShared][kThreads];
+        uint32_t own_bins[kUnits - kShared][kThreads];
     };
-    uint64_t unit_bins[kSpan];
+    uint64_t unit_bins[kUnits];
     Sums warp[kWarps];
     Words warp_words[kWarps];
     Sums peers[2][kMaxCluster];     // exchanges alternate between the two
@@ -467,26 +468,31 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     s.rate = greedy ? 1.f : fminf(__fdiv_rn(0x1.715476p+0f, temperature), 3e38f);
     s.mz = P.minus_zeros;
 
-    // f(two logits, their exponents, index of the first) over this warp's run
+    // f(two logits, index of the first) over this warp's run
     auto each_pair = [&](auto&& f) {
         for (int v = run0 + lane; v < run1; v += 32) {
             float e[kN];
             Vec<T>::split(part[v], e);
 #pragma unroll
-            for (int j = 0; j < kN; j += 2) {
-                float y0, y1;
-                exponents(s, e[j], e[j + 1], y0, y1);
-                f(e[j], e[j + 1], y0, y1, base + v * kN + j);
-            }
+            for (int j = 0; j < kN; j += 2) f(e[j], e[j + 1], base + v * kN + j);
         }
+    };
+    auto weigh = [&](float x0, float x1, float& y0, float& y1, uint32_t& w0, uint32_t& w1) {
+        exponents(s, x0, x1, y0, y1);
+        weights(s, y0, y1, w0, w1);
     };
 
     // ---- bins of y: masses (or counts) of units, then of a unit's kBins parts
-    auto unit_of = [](float y) { return min((int)-y, kSpan - 1); };
+    auto unit_of = [](float y) {
+        const int u = (int)-y;
+        return u < 16 ? u : min(8 + (u >> 1), kUnits - 1);
+    };
+    auto unit_begin = [](int u) { return (float)(u < 16 ? u : 2 * u - 16); };  // -y there
+    auto unit_width = [](int u) { return u < 16 ? 1.f : 2.f; };
     auto clear_units = [&] {
 #pragma unroll
-        for (int i = 0; i < kSpan - kShared; ++i) sm.own_bins[i][tid] = 0;
-        if (tid < kSpan) sm.unit_bins[tid] = 0;
+        for (int i = 0; i < kUnits - kShared; ++i) sm.own_bins[i][tid] = 0;
+        if (tid < kUnits) sm.unit_bins[tid] = 0;
         __syncthreads();
     };
     auto add_to_unit = [&](int unit, uint32_t w) {
@@ -496,7 +502,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     // the block's units, then the cluster's: to every block, in peers' order
     auto join_units = [&] {
         __syncthreads();
-        for (int u = kShared + wid; u < kSpan; u += kWarps) {
+        for (int u = kShared + wid; u < kUnits; u += kWarps) {
             uint64_t m = 0;
             for (int i = lane; i < kThreads; i += 32) m += sm.own_bins[u - kShared][i];
 #pragma unroll
@@ -510,7 +516,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     // does.
     auto find_unit = [&](uint64_t goal, uint64_t& over) {
         uint64_t m = 0;
-        if (lane < kSpan)
+        if (lane < kUnits)
             for (uint32_t b = 0; b < blocks; ++b) m += remote_load64(remote(smem_u32(&sm.unit_bins[lane]), b));
         uint64_t upto = m;
 #pragma unroll
@@ -522,7 +528,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         over = __shfl_sync(~0u, upto - m, max(unit, 0));
         return unit;
     };
-    auto part_index = [&](float y) { return (int)(-y * (float)kBins); };  // of all units' parts
+    // the part of a unit that y lies in: below 0 or from kBins on where it lies above or below the unit
+    auto part_index = [&](float y, int unit) { return (int)floorf((-y - unit_begin(unit)) * ((float)kBins / unit_width(unit))); };
     // the same over the parts of a unit, on top of `over`; a barrier of the cluster stands before
     auto find_part = [&](bool by_mass, uint64_t goal, uint64_t& over) {
         uint64_t m = 0;  // of part `tid`
@@ -551,32 +558,36 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         return (int)sm.found[0];
     };
 
-    // ---- the cut: keys above cut_key, and those equal to it up to cut_index
-    uint32_t cut_key = 1;
+    // ---- the cut: logits above cut_value, and those equal to it up to cut_index
+    constexpr float kLowest = -3.402823466e38f;  // of the finite ones: others are in no cut
+    // a logit below every one whose y is above -units (the rounding of y is 2^-22 of it)
+    auto below_units = [&](float units) { return fmaxf(s.top - (units * 1.00001f + 1e-5f) / s.rate - fabsf(s.top) * 1e-5f, kLowest); };
+    const float weightless = below_units(34.f);   // from it on down
+    float cut_value = weightless;
     int cut_index = P.vocab;
-    auto in_cut = [&](uint32_t key, int i) { return key > cut_key || (key == cut_key && i <= cut_index); };
-    // A unit's parts, of the tokens of the cut with keys >= floor: into sm.bins; the words are the unit's smallest key
+    auto in_cut = [&](float v, int i) { return v > cut_value || (v == cut_value && i <= cut_index); };
+    // A unit's parts, of the tokens of the cut from `floor` on: into sm.bins; the words are the unit's smallest key
     // (complemented) and the number of tokens in it and above it.
-    auto split_unit = [&](bool by_mass, int unit, uint32_t floor) {
+    auto split_unit = [&](bool by_mass, int unit, float floor) {
         for (int i = tid; i < 2 * kBins; i += kThreads) (&sm.bins[0][0])[i] = 0;
         __syncthreads();
-        const int from = unit * kBins;
-        const bool open = unit == kSpan - 1;  // to below
+        floor = fmaxf(floor, below_units(unit_begin(unit) + unit_width(unit)));
         Words v = {0, 0, 0};
-        each_pair([&](float x0, float x1, float y0, float y1, int at) {
-            const float y[2] = {y0, y1}, e[2] = {x0, x1};
+        each_pair([&](float x0, float x1, int at) {
+            if (!(fmaxf(x0, x1) >= floor)) return;
+            float y[2];
+            const float e[2] = {x0, x1};
+            exponents(s, x0, x1, y[0], y[1]);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int b = part_index(y[j]) - from;
-                if (b >= kBins && !open) continue;
-                const uint32_t key = key_of(e[j]);
-                if (key < floor || !in_cut(key, at + j)) continue;
+                const int b = part_index(y[j], unit);
+                if (b >= kBins || !(e[j] >= floor) || !in_cut(e[j], at + j)) continue;
                 ++v.n;
                 if (b < 0) continue;
-                v.high = max(v.high, ~key);
+                v.high = max(v.high, ~key_of(e[j]));
                 const uint32_t w = by_mass ? weight_of(s, e[j]) : 1u;
-                atomicAdd(&sm.bins[0][min(b, kBins - 1)], w & 0xffffu);
-                if (by_mass) atomicAdd(&sm.bins[1][min(b, kBins - 1)], w >> 16);
+                atomicAdd(&sm.bins[0][b], w & 0xffffu);
+                if (by_mass) atomicAdd(&sm.bins[1][b], w >> 16);
             }
         });
         return exchange_words(v);
@@ -585,27 +596,27 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     // `low`; false where there is no room for them (which every block knows).
     auto gather = [&](uint32_t low, uint32_t high, bool few_threads) {
         const uint32_t share = kGather / blocks, to = remote(smem_u32(sm.gather), 0) + 8 * rank * share;
-        auto put = [&](uint32_t key, int at) {
-            if (key < low || key > high || !in_cut(key, at)) return;
+        const float low_value = value_of(low), high_value = value_of(high);
+        auto put = [&](float v, int at) {
+            if (!(v >= low_value && v <= high_value) || !in_cut(v, at)) return;
             const uint32_t slot = atomicAdd(&sm.n_mine, 1u);
-            if (slot < share) remote_store(to + 8 * slot, (uint64_t)key << 32 | (uint32_t)~at);
+            if (slot < share) remote_store(to + 8 * slot, (uint64_t)key_of(v) << 32 | (uint32_t)~at);
         };
         if (few_threads) {
             for (uint32_t m = __ballot_sync(~0u, my_top >= low); m; m &= m - 1) {  // the warp on one thread's logits
                 const int of = __ffs(m) - 1, n = (run1 - run0 - of + 31) / 32 * kN;
                 for (int i = lane; i < n; i += 32) {
                     const int at = (run0 + of + i / kN * 32) * kN + i % kN;
-                    put(key_of(to_float(reinterpret_cast<const T*>(part)[at])), base + at);
+                    put(to_float(reinterpret_cast<const T*>(part)[at]), base + at);
                 }
                 __syncwarp();
             }
         } else {
-            for (int v = run0 + lane; v < run1; v += 32) {
-                float e[kN];
-                Vec<T>::split(part[v], e);
-#pragma unroll
-                for (int j = 0; j < kN; ++j) put(key_of(e[j]), base + v * kN + j);
-            }
+            each_pair([&](float x0, float x1, int at) {
+                if (!(fmaxf(x0, x1) >= low_value)) return;
+                put(x0, at);
+                put(x1, at + 1);
+            });
         }
         __syncthreads();
         if (tid < (int)blocks) remote_store32(remote(smem_u32(&sm.counts[rank]), tid), sm.n_mine);
@@ -653,42 +664,44 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     };
     // The cut goes to the first tokens of the order whose mass (or number) reaches the goal: it lies in `unit`, above
     // which stands `over`, and whose parts are in sm.bins.
-    auto cut_in = [&](bool by_mass, uint64_t goal, uint64_t over, int unit, uint32_t floor) {
-        const int from = unit * kBins + find_part(by_mass, goal, over);
-        const bool open = from == kSpan * kBins - 1;
+    auto cut_in = [&](bool by_mass, uint64_t goal, uint64_t over, int unit, float floor) {
+        const int from = find_part(by_mass, goal, over);
+        floor = fmaxf(floor, below_units(unit_begin(unit) + (float)(from + 1) * (unit_width(unit) / kBins)));
         // the part's largest and smallest key: in between are its tokens alone
         Words v = {0, 0, 0};
-        each_pair([&](float x0, float x1, float y0, float y1, int at) {
-            const int b0 = part_index(y0), b1 = part_index(y1);
-            if (max(b0, b1) < from || (min(b0, b1) > from && !open)) return;
-            const uint32_t k0 = key_of(x0), k1 = key_of(x1);
-            if ((b0 == from || (open && b0 > from)) && k0 >= floor && in_cut(k0, at)) v = Words{max(v.top, k0), max(v.high, ~k0), v.n + 1};
-            if ((b1 == from || (open && b1 > from)) && k1 >= floor && in_cut(k1, at + 1)) v = Words{max(v.top, k1), max(v.high, ~k1), v.n + 1};
+        each_pair([&](float x0, float x1, int at) {
+            if (!(fmaxf(x0, x1) >= floor)) return;
+            float y0, y1;
+            exponents(s, x0, x1, y0, y1);
+            const bool in0 = part_index(y0, unit) == from && x0 >= floor && in_cut(x0, at);
+            const bool in1 = part_index(y1, unit) == from && x1 >= floor && in_cut(x1, at + 1);
+            if (in0) v = Words{max(v.top, key_of(x0)), max(v.high, ~key_of(x0)), 0};
+            if (in1) v = Words{max(v.top, key_of(x1)), max(v.high, ~key_of(x1)), 0};
         });
         v = exchange_words(v);
         uint32_t hi_key = v.top, lo_key = ~v.high;
-        auto weight = [&](uint32_t key) { return by_mass ? weight_of(s, value_of(key)) : 1u; };
         if (lo_key < hi_key && gather(lo_key, hi_key, false)) {
             Words c = {0, 0, 0};  // the token that reaches the goal
-            if (rank == 0) {
-                const uint32_t n = sm.n_list;
-                rank_list(n, weight, [&](int, uint32_t i, uint32_t, uint64_t above) {
-                    if (over + above < goal && goal <= over + above + sm.weight[i]) c = Words{(uint32_t)(sm.list[i] >> 32), ~(uint32_t)sm.list[i] + 1u, 0};
-                });
-            }
+            if (rank == 0)
+                rank_list(sm.n_list, [&](uint32_t key) { return by_mass ? weight_of(s, value_of(key)) : 1u; },
+                          [&](int, uint32_t i, uint32_t, uint64_t above) {
+                              if (over + above < goal && goal <= over + above + sm.weight[i])
+                                  c = Words{(uint32_t)(sm.list[i] >> 32), ~(uint32_t)sm.list[i] + 1u, 0};
+                          });
             c = exchange_words(c);
             if (tid == 0) sm.n_list = 0;
-            cut_key = c.top;
+            cut_value = value_of(c.top);
             cut_index = (int)c.high - 1;
             return;
         }
         uint64_t above = 0;  // of the part, before the cut's key
+        const float part_top = value_of(v.top);
         auto tally_part = [&](uint32_t from_key) {  // the part's keys >= from_key
             Sums t = {0, 0, 0, 0};
-            each_pair([&](float x0, float x1, float, float, int at) {
-                const uint32_t k0 = key_of(x0), k1 = key_of(x1);
-                if (k0 >= from_key && k0 <= v.top && in_cut(k0, at)) t.a += weight(k0);
-                if (k1 >= from_key && k1 <= v.top && in_cut(k1, at + 1)) t.a += weight(k1);
+            const float low = value_of(from_key);
+            each_pair([&](float x0, float x1, int at) {
+                if (x0 >= low && x0 <= part_top && in_cut(x0, at)) t.a += by_mass ? weight_of(s, x0) : 1u;
+                if (x1 >= low && x1 <= part_top && in_cut(x1, at + 1)) t.a += by_mass ? weight_of(s, x1) : 1u;
             });
             return exchange(t, nullptr).a;
         };
@@ -701,12 +714,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             if (lo_key < v.top) above = tally_part(lo_key + 1);
         }
         // of the tokens equal to it, those still needed, by index
-        const uint32_t each = weight(lo_key);
+        const float value = value_of(lo_key);
+        const uint32_t each = by_mass ? weight_of(s, value) : 1u;
         const uint64_t need = (goal - over - above + each - 1) / each;
         uint32_t c = 0;
-        each_pair([&](float x0, float x1, float, float, int at) {
-            c += (key_of(x0) == lo_key && in_cut(lo_key, at)) + (key_of(x1) == lo_key && in_cut(lo_key, at + 1));
-        });
+        each_pair([&](float x0, float x1, int at) { c += (x0 == value && in_cut(value, at)) + (x1 == value && in_cut(value, at + 1)); });
         c = __reduce_add_sync(~0u, c);
         Sums before;
         exchange(Sums{0, 0, 0, lane == 0 ? c : 0u}, &before);
@@ -715,8 +727,8 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         uint32_t index = 0;
         if (seen < need && need <= seen + c) {  // in this warp's run: 32 logits at a time
             for (int i = run0 * kN; i < run1 * kN; i += 32) {
-                const uint32_t key = i + lane < run1 * kN ? key_of(to_float(reinterpret_cast<const T*>(part)[i + lane])) : 0;
-                uint32_t m = __ballot_sync(~0u, key == lo_key && in_cut(key, base + i + lane));
+                const bool is = i + lane < run1 * kN && to_float(reinterpret_cast<const T*>(part)[i + lane]) == value && in_cut(value, base + i + lane);
+                uint32_t m = __ballot_sync(~0u, is);
                 if (seen + __popc(m) < need) {
                     seen += __popc(m);
                     continue;
@@ -727,15 +739,17 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             }
         }
         cut_index = (int)exchange_words(Words{index, 0, 0}).top - 1;  // the goal is reached, so that there is one
-        cut_key = lo_key;
+        cut_value = value;
     };
-    // the cut to the first tokens that reach the goal, among those with keys >= floor; nothing where they do not
-    auto cut_at = [&](bool by_mass, uint64_t goal, uint32_t floor) {
+    // the cut to the first tokens that reach the goal, among those from `floor` on; nothing where they do not
+    auto cut_at = [&](bool by_mass, uint64_t goal, float floor) {
         clear_units();
-        each_pair([&](float x0, float x1, float y0, float y1, int at) {
-            const bool in0 = key_of(x0) >= floor && in_cut(key_of(x0), at), in1 = key_of(x1) >= floor && in_cut(key_of(x1), at + 1);
+        each_pair([&](float x0, float x1, int at) {
+            const bool in0 = x0 >= floor && in_cut(x0, at), in1 = x1 >= floor && in_cut(x1, at + 1);
             if (!in0 && !in1) return;
+            float y0, y1;
             uint32_t w0 = 1, w1 = 1;
+            exponents(s, x0, x1, y0, y1);
             if (by_mass) weights(s, y0, y1, w0, w1);
             if (in0) add_to_unit(unit_of(y0), w0);
             if (in1) add_to_unit(unit_of(y1), w1);
@@ -761,10 +775,11 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         // Weights fall with the logits but for the rounding of the polynomial: `loose` is below every weight that can
         // stand before one of `least` in the order.
         const uint32_t loose = least == 1 ? 0 : least - min(least, (least >> 20) + 1u);
+        float y0, y1;
+        uint32_t w0, w1;
         if (least > 1) {
-            each_pair([&](float, float, float y0, float y1, int) {
-                uint32_t w0, w1;
-                weights(s, y0, y1, w0, w1);
+            each_pair([&](float x0, float x1, int) {
+                weigh(x0, x1, y0, y1, w0, w1);
                 v.a += (uint64_t)w0 + w1;
                 if (max(w0, w1) < loose) return;
                 v.b += (uint64_t)(w0 >= loose ? w0 : 0u) + (w1 >= loose ? w1 : 0u);
@@ -773,18 +788,17 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             });
         } else if (cut) {
             clear_units();
-            each_pair([&](float, float, float y0, float y1, int) {
-                uint32_t w0, w1;
-                weights(s, y0, y1, w0, w1);
+            each_pair([&](float x0, float x1, int) {
+                weigh(x0, x1, y0, y1, w0, w1);
                 v.a += (uint64_t)w0 + w1;
                 add_to_unit(unit_of(y0), w0);
                 add_to_unit(unit_of(y1), w1);
             });
         } else {
-            each_pair([&](float, float, float y0, float y1, int) {
-                uint32_t w0, w1;
-                weights(s, y0, y1, w0, w1);
-                v.c += (uint64_t)w0 + w1;
+            each_pair([&](float x0, float x1, int) {
+                weigh(x0, x1, y0, y1, w0, w1);
+                v.c += w0;
+                v.c += w1;
                 v.n += min(w0, 1u) + min(w1, 1u);
             });
         }
@@ -799,20 +813,19 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             if (least > 1) {  // the nucleus ends above what min-p leaves out: no lower unit than `loose` falls in, or the next
                 clear_units();
                 const int last = unit_of(log2f((float)max(loose, 1u)) - 31.f) + 1;
-                each_pair([&](float, float, float y0, float y1, int) {
-                    const int u0 = unit_of(y0), u1 = unit_of(y1);
-                    if (min(u0, u1) > last) return;
-                    uint32_t w0, w1;
-                    weights(s, y0, y1, w0, w1);
-                    if (u0 <= last) add_to_unit(u0, w0);
-                    if (u1 <= last) add_to_unit(u1, w1);
+                const float floor = last < kUnits - 1 ? below_units(unit_begin(last) + unit_width(last)) : weightless;
+                each_pair([&](float x0, float x1, int) {
+                    if (!(fmaxf(x0, x1) >= floor)) return;
+                    weigh(x0, x1, y0, y1, w0, w1);
+                    if (unit_of(y0) <= last) add_to_unit(unit_of(y0), w0);
+                    if (unit_of(y1) <= last) add_to_unit(unit_of(y1), w1);
                 });
             }
             join_units();
             unit = find_unit(goal, over);
             if (blocks > 1) cluster_sync();  // no block goes on to other bins while another reads these
             else __syncthreads();
-            const Words in = split_unit(true, unit, 1);
+            const Words in = split_unit(true, unit, weightless);
             // few tokens up to the unit's end: no block has more than its share of the list
             by_list = in.n <= (uint32_t)min(kList, (int)(kGather / blocks));
             bound = ~in.high;
@@ -820,7 +833,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     }
 
     // ---- few tokens: the first block has them all
-    if (cut && by_list && gather(bound, 0xffffffffu, true)) {
+    if (cut && by_list && gather(max(bound, key_of(kLowest)), top_key, true)) {
         if (rank != 0) return;
         const uint32_t n = sm.n_list;
         uint64_t above[kRounds], total = 0;
@@ -882,27 +895,29 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
 
     // ---- many: the cut, and what stands before it
     if (cut) {
+        float y0, y1;
+        uint32_t w0, w1;
         if (k != 0xffffffffu) {
-            cut_at(false, k, bound);
+            cut_at(false, k, bound > 1 ? fmaxf(value_of(bound), weightless) : weightless);
             if (p_part < 0x80000000u) {
                 Sums v = {0, 0, 0, 0};
-                each_pair([&](float x0, float x1, float, float, int at) {
-                    v.a += (uint64_t)(in_cut(key_of(x0), at) ? weight_of(s, x0) : 0u) + (in_cut(key_of(x1), at + 1) ? weight_of(s, x1) : 0u);
+                each_pair([&](float x0, float x1, int at) {
+                    if (!(fmaxf(x0, x1) >= cut_value)) return;
+                    weigh(x0, x1, y0, y1, w0, w1);
+                    v.a += (uint64_t)(in_cut(x0, at) ? w0 : 0u) + (in_cut(x1, at + 1) ? w1 : 0u);
                 });
                 goal = max(share_of(exchange(v, nullptr).a, p_part), (uint64_t)1);
-                cut_at(true, goal, cut_key);
+                cut_at(true, goal, cut_value);
             }
         } else {
-            cut_in(true, goal, over, unit, 1);
+            cut_in(true, goal, over, unit, weightless);
         }
         Sums v = {0, 0, 0, 0};
-        each_pair([&](float x0, float x1, float y0, float y1, int at) {
-            const bool in0 = in_cut(key_of(x0), at), in1 = in_cut(key_of(x1), at + 1);
-            if (!in0 && !in1) return;
-            uint32_t w0, w1;
-            weights(s, y0, y1, w0, w1);
-            if (!in0 || w0 < least) w0 = 0;
-            if (!in1 || w1 < least) w1 = 0;
+        each_pair([&](float x0, float x1, int at) {
+            if (!(fmaxf(x0, x1) >= cut_value)) return;
+            weigh(x0, x1, y0, y1, w0, w1);
+            if (!in_cut(x0, at) || w0 < least) w0 = 0;
+            if (!in_cut(x1, at + 1) || w1 < least) w1 = 0;
             v.c += (uint64_t)w0 + w1;
             v.n += min(w0, 1u) + min(w1, 1u);
         });
@@ -922,7 +937,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     const int each = (chunk * kN + kThreads - 1) / kThreads, a0 = min(e0 + tid * each, e1), a1 = min(a0 + each, e1);
     auto kept_weight = [&](int i) {
         const float v = to_float(reinterpret_cast<const T*>(part)[i]);
-        if (cut && !in_cut(key_of(v), base + i)) return 0u;
+        if (cut && !in_cut(v, base + i)) return 0u;
         const uint32_t w = weight_of(s, v);
         return w >= least ? w : 0u;
     };
