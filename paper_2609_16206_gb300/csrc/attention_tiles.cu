@@ -31,7 +31,9 @@ template <int D, int kTiles>
 struct Layout {
     static constexpr int kRows = 128 * kTiles;                 // of an item
     static constexpr int kKeys = kTiles == 1 ? 64 : 128;       // of a unit
-    static constexpr int kThreads = 128 * kTiles + 64;         // softmax warpgroups, a loading warp, an issuing warp
+    // softmax warpgroups, a loading warp, an issuing warp; beside two tiles a whole warpgroup with them, whose registers
+    // the softmax takes over: at launch 384 x 168, then 256 x 216 + 128 x 72, the same sum
+    static constexpr int kThreads = kTiles == 1 ? 192 : 384;
     static constexpr int kBlocksPerSm = kTiles == 1 ? 2 : 1;
     static constexpr int kSlot = kKeys * D * 2;                // bytes of a ring slot: a unit's keys or its values
     static constexpr int kQ = kRows * D * 2;
@@ -204,102 +206,19 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     auto parity_of = [](uint32_t u) { return kTiles == 1 ? u >> 1 & 1 : u & 1; };
     Walk w;
     w.start(P, range, kKeys, L::kRows);
-
-    if (wid == 4 * kTiles) {
-        // ------------------------------------------------ loads: of each unit the keys, then the values
-        const int box = min(P.cache.page_tokens, kKeys), boxes = kKeys / box;
-        uint32_t n = 0, issued = 0;
-        for (; w.more(); w.next(P, kKeys, L::kRows)) {
-            const int head = w.h / (w.items / P.cache.n_kv_heads);
-            for (; w.u < w.end; ++w.u) {
-                const int key = w.u * kKeys + lane * box;
-                int page = -1;  // past the end: reads zeros
-                if (lane < boxes && key < w.s.len) page = __ldg(P.page_table + (int64_t)w.b * P.table_stride + (key >> P.page_log2));
-                for (int v = 0; v < 2; ++v, ++n) {
-                    const uint32_t slot = n % kSlots, at = ring + slot * L::kSlot + lane * box * 128;
-                    if (n >= kSlots) wait_warp(empty + 8 * slot, (n / kSlots + 1) & 1);
-                    if (!fine) continue;
-                    if (lane == 0) bar_expect(full + 8 * slot, L::kSlot);
-                    __syncwarp();
-                    if (lane < boxes) {
-                        const int y = key & (P.cache.page_tokens - 1);
-#pragma unroll
-                        for (int i = 0; i < D / 64; ++i)
-                            tma_load(at + i * kKeys * 128, v ? &map_v : &map_k, full + 8 * slot, 64 * i, y, head, page);
-                    }
-                    issued = n + 1;
-                }
-            }
-        }
-        // every load issued has landed before the block leaves (bounded again where a wait has run out)
-        for (uint32_t i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i) bar_wait(full + 8 * (i % kSlots), (i / kSlots) & 1);
-    } else if (wid == 4 * kTiles + 1) {
-        // ------------------------------------------------ products, issued by one thread
-        if (lane == 0) {
-            constexpr uint32_t kScores = instruction<T>(false, kKeys), kValues = instruction<T>(true, D);
-            uint32_t n = 0, items = 0, units = 0;  // ring slots used, items and units begun
-            auto scores = [&](int t, uint32_t slot, int region) {
-                const uint32_t q = base + t * 128 * D * 2, k = ring + slot * L::kSlot;
-#pragma unroll
-                for (int i = 0; i < D / 16; ++i)
-                    mma_shared(tmem + region * kKeys, operand(q + (i >> 2) * 128 * 128 + (i & 3) * 32, 16),
-                               operand(k + (i >> 2) * kKeys * 128 + (i & 3) * 32, 16), kScores, i > 0);
-                mma_commit(s_full + 8 * region);
-            };
-            auto values = [&](int t, uint32_t slot, int region, bool add) {
-                const uint32_t v = ring + slot * L::kSlot;
-#pragma unroll
-                for (int i = 0; i < kKeys / 16; ++i)
-                    mma_tensor(tmem + L::kO + t * D, tmem + region * kKeys + 8 * i, operand(v + i * 2048, kKeys * 128), kValues, add || i > 0);
-                mma_commit(o_full + 8 * t);
-            };
-            for (; w.more(); w.next(P, kKeys, L::kRows), ++items) {
-                const int count = w.end - w.begin;
-                for (int t = 0; t < kTiles; ++t) wait_thread(q_full + 8 * t, items & 1);
-                if (!wait_thread(full + 8 * (n % kSlots), (n / kSlots) & 1)) continue;
-                fence_after();
-                for (int t = 0; t < kTiles; ++t) scores(t, n % kSlots, region_of(t, units));
-                mma_commit(empty + 8 * (n % kSlots));
-                for (int i = 0; i < count && fine; ++i, n += 2, ++units) {
-                    // the next unit's scores go ahead of this one's values where they have a region of their own (one
-                    // tile), else right behind each tile's values: the softmax of one tile runs beside the other's products
-                    const uint32_t next = n + 2, value_slot = (n + 1) % kSlots;
-                    const bool more = i + 1 < count;
-                    auto wait_next = [&]() {
-                        const bool ok = wait_thread(full + 8 * (next % kSlots), (next / kSlots) & 1);
-                        fence_after();
-                        return ok;
-                    };
-                    if (kTiles == 1 && more) {
-                        if (!wait_next()) break;
-                        scores(0, next % kSlots, region_of(0, units + 1));
-                        mma_commit(empty + 8 * (next % kSlots));
-                    }
-                    for (int t = 0; t < kTiles; ++t) {
-                        if (!wait_thread(p_full + 8 * region_of(t, units), parity_of(units))) break;
-                        if (t == 0 && !wait_thread(full + 8 * value_slot, ((n + 1) / kSlots) & 1)) break;
-                        fence_after();
-                        values(t, value_slot, region_of(t, units), i > 0);
-                        if (t == kTiles - 1) mma_commit(empty + 8 * value_slot);
-                        if (kTiles > 1 && more) {
-                            if (t == 0 && !wait_next()) break;
-                            scores(t, next % kSlots, t);
-                            if (t == kTiles - 1) mma_commit(empty + 8 * (next % kSlots));
-                        }
-                    }
-                }
-            }
-            mma_commit(done);  // every product is done before the tensor memory is given back
-            bar_wait(done, 0);
-        }
-        __syncwarp();
-    } else {
+    // an item's tiles with rows
+    auto tiles_of = [&](const Walk& at) {
+        const int groups = at.items / P.cache.n_kv_heads;
+        return kTiles == 1 || at.s.n_new * P.group - at.h % groups * L::kRows <= 128 ? 1 : 2;
+    };
+    if (wid < 4 * kTiles) {
+        if (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ------------------------------------------------ softmax: a row a thread
         const int tile = wid >> 2, r = tid & 127;
         const uint32_t lanes = (uint32_t)(32 * (wid & 3)) << 16;
         const uint32_t o_at = tmem + lanes + L::kO + tile * D;
         const float scale = P.scale_log2 == 0.f ? 1.f : fabsf(P.scale_log2);
-        uint32_t units = 0, items = 0;
+        uint32_t units = 0, block_units = 0, items = 0;  // of the tile; of the block; items of the block
         for (; w.more(); w.next(P, kKeys, L::kRows), ++items) {
             const int groups = w.items / P.cache.n_kv_heads, head = w.h / groups;
             const int row = (w.h - head * groups) * L::kRows + tile * 128 + r;
@@ -310,6 +229,10 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             // all rows begin an item together: no thread still reads the word of bad tokens that the next item takes
             asm volatile("bar.sync 1, %0;" ::"r"(128 * kTiles) : "memory");
             if (tid == 0) bad_tokens[(items + 1) & 1] = 0;
+            if (tile >= tiles_of(w)) {
+                block_units += w.end - w.begin;
+                continue;
+            }
             {
                 // The queries of this row; the last scores of the item before are done.  A negative scale turns them round,
                 // a scale of 0 is a query of zeros: the factor that the maxima and exponents take is positive.
@@ -328,7 +251,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 bar_arrive(q_full + 8 * tile);
             }
             float top = -INFINITY, sum = 0.f;  // top: what the exponents are relative to, 2^-kLift of the largest
-            for (; w.u < w.end; ++w.u, ++units) {
+            for (; w.u < w.end; ++w.u, ++units, ++block_units) {
                 const int key = w.u * kKeys;
                 const int region = region_of(tile, units);
                 const uint32_t s_at = tmem + lanes + region * kKeys;
@@ -377,24 +300,26 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     }
                 }
                 const float ref = top == -INFINITY ? 0.f : top;
-                float part[4] = {0.f, 0.f, 0.f, 0.f};
+                const uint64_t scale2 = pack(scale, scale), ref2 = pack(-ref, -ref);
+                uint64_t part[2] = {0, 0};
 #pragma unroll
                 for (int c = 0; c < kKeys / 64; ++c) {
                     uint32_t x[32];
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
-                        const float a = exp2_fast(fmaf(s[64 * c + 2 * i], scale, -ref)), b = exp2_fast(fmaf(s[64 * c + 2 * i + 1], scale, -ref));
-                        part[(2 * i) & 3] += a;
-                        part[(2 * i + 1) & 3] += b;
+                        const uint64_t e = fma2(pack(s[64 * c + 2 * i], s[64 * c + 2 * i + 1]), scale2, ref2);
+                        const float a = exp2_fast(low_of(e)), b = exp2_fast(high_of(e));
+                        part[i & 1] = add2(part[i & 1], pack(a, b));
                         x[i] = Pair<T>::join(a, b);
                     }
                     tmem_store(s_at + 32 * c, x);
                 }
-                sum += (part[0] + part[1]) + (part[2] + part[3]);
+                const uint64_t all = add2(part[0], part[1]);
+                sum += low_of(all) + high_of(all);
                 if (edge && tile == 0) {
                     // Values that no row may see, or only some: those past the end become zeros, and a new token's that are
                     // not finite too, to be added at the end to the rows that attend to it.
-                    const uint32_t n = 2 * units + 1, slot = n % kSlots;
+                    const uint32_t n = 2 * block_units + 1, slot = n % kSlots;
                     if (wait_warp(full + 8 * slot, (n / kSlots) & 1) && r < kKeys) {
                         unsigned char* values = smem + L::kRing + slot * L::kSlot;
                         const int p = key + r, new_token = p - w.s.context;
@@ -485,6 +410,100 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 split_slots(P)[blockIdx.x] = d;
             }
             fence_before();
+        }
+    } else {
+        if (kTiles == 2) asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+        if (wid == 4 * kTiles) {
+            // ------------------------------------------------ loads: of each unit the keys, then the values
+            const int box = min(P.cache.page_tokens, kKeys), boxes = kKeys / box;
+            uint32_t n = 0, issued = 0;
+            for (; w.more(); w.next(P, kKeys, L::kRows)) {
+                const int head = w.h / (w.items / P.cache.n_kv_heads);
+                for (; w.u < w.end; ++w.u) {
+                    const int key = w.u * kKeys + lane * box;
+                    int page = -1;  // past the end: reads zeros
+                    if (lane < boxes && key < w.s.len) page = __ldg(P.page_table + (int64_t)w.b * P.table_stride + (key >> P.page_log2));
+                    for (int v = 0; v < 2; ++v, ++n) {
+                        const uint32_t slot = n % kSlots, at = ring + slot * L::kSlot + lane * box * 128;
+                        if (n >= kSlots) wait_warp(empty + 8 * slot, (n / kSlots + 1) & 1);
+                        if (!fine) continue;
+                        if (lane == 0) bar_expect(full + 8 * slot, L::kSlot);
+                        __syncwarp();
+                        if (lane < boxes) {
+                            const int y = key & (P.cache.page_tokens - 1);
+#pragma unroll
+                            for (int i = 0; i < D / 64; ++i)
+                                tma_load(at + i * kKeys * 128, v ? &map_v : &map_k, full + 8 * slot, 64 * i, y, head, page);
+                        }
+                        issued = n + 1;
+                    }
+                }
+            }
+            // every load issued has landed before the block leaves (bounded again where a wait has run out)
+            for (uint32_t i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i) bar_wait(full + 8 * (i % kSlots), (i / kSlots) & 1);
+        } else if (wid == 4 * kTiles + 1) {
+            // ------------------------------------------------ products, issued by one thread
+            if (lane == 0) {
+                constexpr uint32_t kScores = instruction<T>(false, kKeys), kValues = instruction<T>(true, D);
+                uint32_t n = 0, items[2] = {0, 0}, units[2] = {0, 0};  // ring slots used; a tile's items and units begun
+                auto scores = [&](int t, uint32_t slot, int region) {
+                    const uint32_t q = base + t * 128 * D * 2, k = ring + slot * L::kSlot;
+#pragma unroll
+                    for (int i = 0; i < D / 16; ++i)
+                        mma_shared(tmem + region * kKeys, operand(q + (i >> 2) * 128 * 128 + (i & 3) * 32, 16),
+                                   operand(k + (i >> 2) * kKeys * 128 + (i & 3) * 32, 16), kScores, i > 0);
+                    mma_commit(s_full + 8 * region);
+                };
+                auto values = [&](int t, uint32_t slot, int region, bool add) {
+                    const uint32_t v = ring + slot * L::kSlot;
+#pragma unroll
+                    for (int i = 0; i < kKeys / 16; ++i)
+                        mma_tensor(tmem + L::kO + t * D, tmem + region * kKeys + 8 * i, operand(v + i * 2048, kKeys * 128), kValues, add || i > 0);
+                    mma_commit(o_full + 8 * t);
+                };
+                for (; w.more(); w.next(P, kKeys, L::kRows)) {
+                    const int count = w.end - w.begin, tiles = tiles_of(w);
+                    for (int t = 0; t < tiles; ++t) wait_thread(q_full + 8 * t, items[t]++ & 1);
+                    if (!wait_thread(full + 8 * (n % kSlots), (n / kSlots) & 1)) continue;
+                    fence_after();
+                    for (int t = 0; t < tiles; ++t) scores(t, n % kSlots, region_of(t, units[t]));
+                    mma_commit(empty + 8 * (n % kSlots));
+                    for (int i = 0; i < count && fine; ++i, n += 2) {
+                        // the next unit's scores go ahead of this one's values where they have a region of their own (one
+                        // tile), else right behind each tile's values: the softmax of one tile runs beside the other's products
+                        const uint32_t next = n + 2, value_slot = (n + 1) % kSlots;
+                        const bool more = i + 1 < count;
+                        auto wait_next = [&]() {
+                            const bool ok = wait_thread(full + 8 * (next % kSlots), (next / kSlots) & 1);
+                            fence_after();
+                            return ok;
+                        };
+                        if (kTiles == 1 && more) {
+                            if (!wait_next()) break;
+                            scores(0, next % kSlots, region_of(0, units[0] + 1));
+                            mma_commit(empty + 8 * (next % kSlots));
+                        }
+#pragma unroll
+                        for (int t = 0; t < kTiles; ++t) {
+                            if (t >= tiles) break;
+                            if (!wait_thread(p_full + 8 * region_of(t, units[t]), parity_of(units[t]))) break;
+                            if (t == 0 && !wait_thread(full + 8 * value_slot, ((n + 1) / kSlots) & 1)) break;
+                            fence_after();
+                            values(t, value_slot, region_of(t, units[t]), i > 0);
+                            ++units[t];
+                            if (t == tiles - 1) mma_commit(empty + 8 * value_slot);
+                            if (kTiles > 1 && more) {
+                                if (t == 0 && !wait_next()) break;
+                                scores(t, next % kSlots, t);
+                                if (t == tiles - 1) mma_commit(empty + 8 * (next % kSlots));
+                            }
+                        }
+                    }
+                }
+                mma_commit(done);  // every product is done before the tensor memory is given back
+                bar_wait(done, 0);
+            }
+            __syncwarp();
         }
     }
     __syncthreads();

@@ -51,20 +51,6 @@ __device__ __forceinline__ float value_of(uint32_t key)
 }
 
 // ---------------------------------------------------------------- weights
-__device__ __forceinline__ uint64_t pack(float a, float b) { return (uint64_t)__float_as_uint(b) << 32 | __float_as_uint(a); }
-__device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
-{
-    uint64_t r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-
 // What a row's weights need: its maximum, the rate, and the two fp32 -0 that make a fused multiply-add a product
 // rounded on its own (from the kernel's parameters: a plain product the assembler contracts into the sum behind it).
 struct Scale {
@@ -76,8 +62,8 @@ struct Scale {
 __device__ __forceinline__ void exponents(const Scale& s, float x0, float x1, float& y0, float& y1)
 {
     const uint64_t y = fma2(add2(pack(x0, x1), pack(-s.top, -s.top)), pack(s.rate, s.rate), s.mz);
-    y0 = fmaxf(__uint_as_float((uint32_t)y), -64.f);
-    y1 = fmaxf(__uint_as_float((uint32_t)(y >> 32)), -64.f);
+    y0 = fmaxf(low_of(y), -64.f);
+    y1 = fmaxf(high_of(y), -64.f);
 }
 
 // round(2^31 2^y): y = k + f with k its nearest integer (by adding 1.5 2^23 + 32, whose low bits are then k + 32), 2^f =
