@@ -61,19 +61,25 @@ __device__ __forceinline__ void bar_arrive(uint32_t bar)
 {
     asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory");
 }
+__device__ __forceinline__ bool bar_try(uint32_t bar, uint32_t parity)
+{
+    uint32_t done;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(done)
+        : "r"(bar), "r"(parity)
+        : "memory");
+    return done != 0;
+}
 // false where the bound ran out
 __device__ __forceinline__ bool bar_wait(uint32_t bar, uint32_t parity)
 {
-    uint32_t done = 0;
-    for (unsigned it = 0; it < kWaitLimit && !done; ++it)
-        asm volatile(
-            "{\n\t.reg .pred p;\n\t"
-            "mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
-            "selp.u32 %0, 1, 0, p;\n\t}"
-            : "=r"(done)
-            : "r"(bar), "r"(parity)
-            : "memory");
-    return done != 0;
+    if (bar_try(bar, parity)) return true;
+    for (unsigned it = 0; it < kWaitLimit; ++it)
+        if (bar_try(bar, parity)) return true;
+    return false;
 }
 // a box of a cache's map: 64 dimensions from x (0 or 64), tokens of a page from y, one head, one page
 __device__ __forceinline__ void tma_load(uint32_t dst, const CUtensorMap* map, uint32_t bar, int x, int y, int head, int page)
@@ -238,7 +244,8 @@ struct Walk {
 };
 
 // Workspace: blocks SplitSlots, then per block and slot the partial sums of up to `rows` rows: their maxima and
-// weight sums, and `rows` x head_dim fp32 outputs.
+// weight sums, and `rows` x head_dim fp32 outputs, row by row, or (columns) the rows of each head_dim / 32 dimensions
+// together, as a kernel with a row a thread writes them.
 __host__ __device__ __forceinline__ size_t slots_bytes(int blocks) { return ((size_t)blocks * sizeof(SplitSlot) + 255) / 256 * 256; }
 __host__ __device__ __forceinline__ size_t part_floats(int rows, int d) { return (size_t)rows * (d + 2); }
 __device__ __forceinline__ SplitSlot* split_slots(const AttentionParams& P) { return reinterpret_cast<SplitSlot*>(P.ws); }
@@ -248,7 +255,7 @@ __device__ __forceinline__ float* part_of_item(const AttentionParams& P, int blo
 }
 
 cudaError_t make_cache_maps(const AttentionParams& p, int box_tokens, CUtensorMap* k, CUtensorMap* v);
-cudaError_t launch_merge(const AttentionParams& p, int blocks, int rows, cudaStream_t stream);
+cudaError_t launch_merge(const AttentionParams& p, int blocks, int rows, bool columns, cudaStream_t stream);
 
 int sm_count();  // of the current device
 size_t stream_workspace(int rows, int d);

@@ -425,7 +425,7 @@ cudaError_t launch(const AttentionParams& p, cudaStream_t stream)
     const int blocks = sm_count() * L::kBlocksPerSm;
     err = launch_dependent(kernel, dim3(blocks), dim3(kThreads), bytes, 1, stream, k, v, p);
     if (err != cudaSuccess) return err;
-    return launch_merge(p, blocks, L::kRows, stream);
+    return launch_merge(p, blocks, L::kRows, false, stream);
 }
 
 template <typename T>

@@ -30,25 +30,25 @@ template <> struct Lift<__half> { static constexpr float k = 7.f; };
 template <int D, int kTiles>
 struct Layout {
     static constexpr int kRows = 128 * kTiles;                 // of an item
-    static constexpr int kKeys = kTiles == 1 ? 64 : 128;       // of a unit
+    static constexpr int kKeys = 64;                           // of a unit
     // softmax warpgroups, a loading warp, an issuing warp; beside two tiles a whole warpgroup with them, whose registers
     // the softmax takes over: at launch 384 x 168, then 256 x 216 + 128 x 72, the same sum
     static constexpr int kThreads = kTiles == 1 ? 192 : 384;
     static constexpr int kBlocksPerSm = kTiles == 1 ? 2 : 1;
     static constexpr int kSlot = kKeys * D * 2;                // bytes of a ring slot: a unit's keys or its values
     static constexpr int kQ = kRows * D * 2;
-    static constexpr int kSlots = kTiles == 1 ? 5 : (D == 128 ? 5 : 8);
+    static constexpr int kSlots = kTiles == 1 ? 5 : 10;
     static constexpr int kRing = kQ;
-    // full [kSlots], empty [kSlots]; scores and probabilities of either region [2] each; queries and outputs of a tile
-    // [2] each; one for the end
+    // full [kSlots], empty [kSlots]; a tile's queries [2]; scores, probabilities and products with the values of a tile's
+    // even and odd units [4] each; one for the end
     static constexpr int kBars = kRing + kSlots * kSlot;
-    static constexpr int kNBars = 2 * kSlots + 9;
+    static constexpr int kNBars = 2 * kSlots + 15;
     static constexpr int kScratch = kBars + kNBars * 8;
     static constexpr int kBad = kScratch + (kThreads / 32 + 2) * 8;  // two words of new tokens with values not finite
     static constexpr int kTmem = kBad + 16;
     static constexpr int kBytes = kTmem + 16;
-    static constexpr int kColumns = kTiles == 1 ? 256 : 512;   // of tensor memory: two regions of scores, then outputs
-    static constexpr int kO = 2 * kKeys;
+    static constexpr int kColumns = kTiles == 1 ? 256 : 512;   // of tensor memory: two regions of scores a tile, then outputs
+    static constexpr int kO = 2 * kTiles * kKeys;
 };
 
 // byte offset of 16-byte piece c (of D / 8) of row r in a tile of `rows` rows: halves of 64 dimensions, 128-byte
@@ -59,13 +59,12 @@ __device__ __forceinline__ uint32_t piece(int rows, int r, int c)
 }
 
 // ---------------------------------------------------------------- tcgen05
-// A shared-memory operand with 128-byte swizzle: start, the stride between 64-element blocks of a row-contiguous
-// (MN-major) operand, the stride between groups of 8 rows (1,024 bytes).
-__device__ __forceinline__ uint64_t operand(uint32_t addr, uint32_t block_stride)
-{
-    return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)(block_stride >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | 1ull << 46 |
-           2ull << 61;
-}
+// A shared-memory operand with 128-byte swizzle: its low word, with the start and the stride between 64-element blocks
+// of a row-contiguous (MN-major) operand; the high one has the stride between groups of 8 rows (1,024 bytes).
+__device__ __forceinline__ uint32_t operand(uint32_t addr, uint32_t block_stride) { return (addr & 0x3ffffu) >> 4 | (block_stride >> 4) << 16; }
+constexpr uint32_t kOperandHigh = (1024 >> 4) | 1u << 14 | 2u << 29;
+// The same word in every lane: what the products take has to lie in uniform registers, where offsets are added for free.
+__device__ __forceinline__ uint32_t uniform(uint32_t v) { return __reduce_or_sync(~0u, v); }
 // kind::f16 with fp32 accumulators, M = 128: types of A and B, whether B is MN-major, N
 template <typename T>
 __host__ __device__ constexpr uint32_t instruction(bool b_mn_major, int n)
@@ -73,26 +72,34 @@ __host__ __device__ constexpr uint32_t instruction(bool b_mn_major, int n)
     const uint32_t type = std::is_same<T, __nv_bfloat16>::value ? 1u : 0u;
     return 1u << 4 | type << 7 | type << 10 | (b_mn_major ? 1u << 16 : 0u) | (uint32_t)(n >> 3) << 17 | (uint32_t)(128 >> 4) << 24;
 }
-__device__ __forceinline__ void mma_shared(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add)
+// (the whole warp calls these, one thread issues)
+__device__ __forceinline__ void mma_shared(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        "{\n\t.reg .pred p, one;\n\t.reg .b64 a, b;\n\t"
+        "mov.b64 a, {%1, %5};\n\tmov.b64 b, {%2, %5};\n\t"
+        "setp.ne.u32 p, %4, 0;\n\telect.sync _|one, 0xffffffff;\n\t"
+        "@one tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kOperandHigh)
         : "memory");
 }
-__device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add)
+__device__ __forceinline__ void mma_tensor(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, bool add)
 {
     asm volatile(
-        "{\n\t.reg .pred p;\n\tsetp.ne.u32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d),
-        "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add)
+        "{\n\t.reg .pred p, one;\n\t.reg .b64 b;\n\t"
+        "mov.b64 b, {%2, %5};\n\t"
+        "setp.ne.u32 p, %4, 0;\n\telect.sync _|one, 0xffffffff;\n\t"
+        "@one tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %3, p;\n\t}" ::"r"(d),
+        "r"(a), "r"(b), "r"(idesc), "r"((uint32_t)add), "r"(kOperandHigh)
         : "memory");
 }
 // arrives on the barrier once every product issued before is done
 __device__ __forceinline__ void mma_commit(uint32_t bar)
 {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile(
+        "{\n\t.reg .pred one;\n\telect.sync _|one, 0xffffffff;\n\t"
+        "@one tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar)
+        : "memory");
 }
 __device__ __forceinline__ void fence_after() { asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory"); }
 __device__ __forceinline__ void fence_before() { asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory"); }
@@ -155,20 +162,23 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     constexpr int kKeys = L::kKeys, kSlots = L::kSlots;
     extern __shared__ __align__(1024) unsigned char smem[];
     const uint32_t base = smem_u32(smem), ring = base + L::kRing, full = base + L::kBars, empty = full + 8 * kSlots;
-    const uint32_t q_full = empty + 8 * kSlots, s_full = q_full + 16, p_full = s_full + 16, o_full = p_full + 16, done = o_full + 16;
+    const uint32_t q_full = empty + 8 * kSlots, s_full = q_full + 16, p_full = s_full + 32, o_full = p_full + 32, done = o_full + 32;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     volatile uint32_t* tmem_at = reinterpret_cast<volatile uint32_t*>(smem + L::kTmem);
     unsigned long long* bad_tokens = reinterpret_cast<unsigned long long*>(smem + L::kBad);
 
     if (tid == 0) {
-        for (int i = 0; i < 2 * kSlots; ++i) bar_init(full + 8 * i, 1);
-        for (int i = 0; i < 2; ++i) {
-            bar_init(q_full + 8 * i, 128);
+        for (int i = 0; i < kSlots; ++i) {
+            bar_init(full + 8 * i, 1);
+            bar_init(empty + 8 * i, kTiles);
+        }
+        for (int i = 0; i < 2; ++i) bar_init(q_full + 8 * i, 4);  // a warp's arrival each
+        for (int i = 0; i < 4; ++i) {
             bar_init(s_full + 8 * i, 1);
-            bar_init(p_full + 8 * i, 128);
+            bar_init(p_full + 8 * i, 4);
             bar_init(o_full + 8 * i, 1);
         }
-        bar_init(done, 1);
+        bar_init(done, kTiles);
         bad_tokens[0] = bad_tokens[1] = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_k) : "memory");
@@ -188,22 +198,19 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     fence_after();
     const uint32_t tmem = *tmem_at;
 
-    bool fine = true;  // no wait of this warp (thread, where one thread acts) has run out: after one has, it only walks to the end
-    auto wait_thread = [&](uint32_t bar, uint32_t parity) {
+    // A wait that runs out (never expected) is reported, and the thread waits no more: what it goes on to compute is
+    // unspecified, and it comes to its end.
+    bool fine = true;
+    auto wait = [&](uint32_t bar, uint32_t parity) {
         if (fine && !bar_wait(bar, parity)) {
             fine = false;
             if (P.status) atomicExch(P.status, CTR_ETIMEOUT);
         }
-        return fine;
     };
-    auto wait_warp = [&](uint32_t bar, uint32_t parity) {
-        wait_thread(bar, parity);
-        return fine = __all_sync(~0u, fine);
-    };
-    // Scores and probabilities of unit u (of the block) of a tile: two tiles have a region each, one tile takes the two
-    // in turn, so that the next unit's scores need not wait for this one's softmax.
-    auto region_of = [](int tile, uint32_t u) { return kTiles == 1 ? (int)(u & 1) : tile; };
-    auto parity_of = [](uint32_t u) { return kTiles == 1 ? u >> 1 & 1 : u & 1; };
+    // Scores and probabilities of unit u of a tile take its two regions in turn: the next unit's scores need not wait for
+    // this one's softmax, nor a softmax for scores.
+    auto region_of = [](int tile, uint32_t u) { return 2 * tile + (int)(u & 1); };
+    auto parity_of = [](uint32_t u) { return u >> 1 & 1; };
     Walk w;
     w.start(P, range, kKeys, L::kRows);
     // an item's tiles with rows
@@ -234,29 +241,40 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 continue;
             }
             {
-                // The queries of this row; the last scores of the item before are done.  A negative scale turns them round,
-                // a scale of 0 is a query of zeros: the factor that the maxima and exponents take is positive.
-                const T* src = static_cast<const T*>(P.q.ptr) + at * P.q.token_stride + q_head * P.q.head_stride;
+                // The warp's 32 queries, a row to D / 8 neighbouring lanes; the last scores of the item before are done.  A
+                // negative scale turns them round, a scale of 0 is a query of zeros: the factor that the maxima and
+                // exponents take is positive.
+                constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
                 const uint32_t turn = P.scale_log2 < 0.f ? 0x80008000u : 0u;
-                uint4 v[D / 8];
+                const int row0 = (w.h - head * groups) * L::kRows + 32 * wid, c = lane % kLanes;
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) v[c] = is ? __ldg(reinterpret_cast<const uint4*>(src) + c) : make_uint4(0, 0, 0, 0);
+                for (int i = 0; i < 32 / kAtOnce; i += 8) {
+                    uint4 v[8];
 #pragma unroll
-                for (int c = 0; c < D / 8; ++c) {
-                    v[c].x ^= turn, v[c].y ^= turn, v[c].z ^= turn, v[c].w ^= turn;
-                    if (P.scale_log2 == 0.f) v[c] = make_uint4(0, 0, 0, 0);
-                    *reinterpret_cast<uint4*>(smem + tile * 128 * D * 2 + piece(128, r, c)) = v[c];
+                    for (int j = 0; j < 8; ++j) {
+                        const int q = row0 + (i + j) * kAtOnce + lane / kLanes, n = node_of(P, q);
+                        const T* src = static_cast<const T*>(P.q.ptr) + (w.s.row0 + n) * P.q.token_stride + (int64_t)(head * P.group + q - n * P.group) * P.q.head_stride;
+                        v[j] = q < w.s.n_new * P.group && P.scale_log2 != 0.f ? __ldg(reinterpret_cast<const uint4*>(src) + c) : make_uint4(0, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        v[j].x ^= turn, v[j].y ^= turn, v[j].z ^= turn, v[j].w ^= turn;
+                        *reinterpret_cast<uint4*>(smem + tile * 128 * D * 2 + piece(128, 32 * (wid & 3) + (i + j) * kAtOnce + lane / kLanes, c)) = v[j];
+                    }
                 }
                 fence_async();
-                bar_arrive(q_full + 8 * tile);
+                __syncwarp();
+                if (lane == 0) bar_arrive(q_full + 8 * tile);
             }
             float top = -INFINITY, sum = 0.f;  // top: what the exponents are relative to, 2^-kLift of the largest
             for (; w.u < w.end; ++w.u, ++units, ++block_units) {
                 const int key = w.u * kKeys;
                 const int region = region_of(tile, units);
                 const uint32_t s_at = tmem + lanes + region * kKeys;
+                const bool edge = key + kKeys > w.s.context;
                 float s[kKeys];
-                if (!wait_warp(s_full + 8 * region, parity_of(units))) continue;
+                wait(s_full + 8 * region, parity_of(units));
+                __syncwarp();
                 fence_after();
 #pragma unroll
                 for (int c = 0; c < kKeys / 64; ++c) {
@@ -265,7 +283,6 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
 #pragma unroll
                     for (int i = 0; i < 64; ++i) s[64 * c + i] = __uint_as_float(x[i]);
                 }
-                const bool edge = key + kKeys > w.s.context;
                 if (edge) {
 #pragma unroll
                     for (int c = 0; c < kKeys / 32; ++c) {
@@ -287,7 +304,9 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         top = high;
                         sum *= fix;
                     }
-                    if (!first && wait_warp(o_full + 8 * tile, (units - 1) & 1)) {  // the values of the unit before
+                    if (!first) {  // the unit before's product with the values is done
+                        wait(o_full + 8 * region_of(tile, units - 1), parity_of(units - 1));
+                        __syncwarp();
                         fence_after();
 #pragma unroll
                         for (int c = 0; c < D / 32; ++c) {
@@ -320,7 +339,8 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     // Values that no row may see, or only some: those past the end become zeros, and a new token's that are
                     // not finite too, to be added at the end to the rows that attend to it.
                     const uint32_t n = 2 * block_units + 1, slot = n % kSlots;
-                    if (wait_warp(full + 8 * slot, (n / kSlots) & 1) && r < kKeys) {
+                    wait(full + 8 * slot, (n / kSlots) & 1);
+                    if (r < kKeys) {
                         unsigned char* values = smem + L::kRing + slot * L::kSlot;
                         const int p = key + r, new_token = p - w.s.context;
                         if (p >= w.s.len) {
@@ -345,23 +365,29 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     }
                     fence_async();
                 }
-                // no tile gets two products with its values ahead: a parity tells the last one's end from the one before
-                if (!first) wait_warp(o_full + 8 * tile, (units - 1) & 1);
+                // the other tile's product with these values has to find them like that
+                if (kTiles == 2 && edge && tiles_of(w) == 2) asm volatile("bar.sync 2, 256;" ::: "memory");
+                // a barrier's parity tells an end from the one before, no more: the last but one unit's values are done
+                if (units >= 2) wait(o_full + 8 * region, parity_of(units - 2));
                 tmem_wait_store();
                 fence_before();
-                bar_arrive(p_full + 8 * region);
+                __syncwarp();
+                if (lane == 0) bar_arrive(p_full + 8 * region);
             }
             // the sums of this part of the item
-            wait_warp(o_full + 8 * tile, (units - 1) & 1);
+            wait(o_full + 8 * region_of(tile, units - 1), parity_of(units - 1));
+            __syncwarp();
             fence_after();
             const bool whole = w.begin == 0 && w.end == w.units;
             const float inv = whole ? (sum > 0.f ? 1.f / sum : 0.f) : 1.f;
             const uint64_t bad = is && fine ? bad_tokens[items & 1] & mask : 0;
             float* part = part_of_item(P, gridDim.x, L::kRows, D, blockIdx.x, w.begin == 0 ? 1 : 0);
             const int part_row = tile * 128 + r;
+            unsigned char* stage = smem + tile * 128 * D * 2;  // the queries' place: their last scores are done
 #pragma unroll
             for (int c = 0; c < D / 32; ++c) {
                 uint32_t x[32];
+                __syncwarp();
                 tmem_load(x, o_at + 32 * c);
                 for (uint64_t todo = bad; __builtin_expect(todo != 0, 0); todo &= todo - 1) {  // from the cache
                     const int p = w.s.context + __ffsll(todo) - 1;
@@ -374,26 +400,42 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         if (!(fabsf(f) < INFINITY)) x[i] = __float_as_uint(__uint_as_float(x[i]) + f);
                     }
                 }
-                if (is && fine) {
-                    if (whole) {
-                        uint4* to = reinterpret_cast<uint4*>(static_cast<T*>(P.out.ptr) + at * P.out.token_stride + q_head * P.out.head_stride + 32 * c);
+                if (whole) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t v[4];
+                    for (int i = 0; i < 4; ++i) {
+                        uint32_t v[4];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                v[j] = Pair<T>::join(__uint_as_float(x[8 * i + 2 * j]) * inv, __uint_as_float(x[8 * i + 2 * j + 1]) * inv);
-                            to[i] = make_uint4(v[0], v[1], v[2], v[3]);
-                        }
-                    } else {
-                        uint4* to = reinterpret_cast<uint4*>(part + 2 * L::kRows + (size_t)part_row * D + 32 * c);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) to[i] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                        for (int j = 0; j < 4; ++j)
+                            v[j] = Pair<T>::join(__uint_as_float(x[8 * i + 2 * j]) * inv, __uint_as_float(x[8 * i + 2 * j + 1]) * inv);
+                        *reinterpret_cast<uint4*>(stage + piece(128, r, 4 * c + i)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
+                } else if (is) {
+                    constexpr int kPer = D / 32;  // dimensions of a lane of the merge
+                    float* to = part + 2 * L::kRows + (32 * c / kPer * L::kRows + part_row) * kPer;
+#pragma unroll
+                    for (int i = 0; i < 32 / kPer; ++i) {
+                        if constexpr (kPer == 4)
+                            *reinterpret_cast<uint4*>(to + i * L::kRows * kPer) = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
+                        else
+                            *reinterpret_cast<uint2*>(to + i * L::kRows * kPer) = make_uint2(x[2 * i], x[2 * i + 1]);
+                    }
+                }
+            }
+            if (whole) {  // the warp's rows, whole ones at a time
+                __syncwarp();
+                constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
+                const int row0 = (w.h - head * groups) * L::kRows + 32 * wid, c = lane % kLanes;
+#pragma unroll 4
+                for (int i = 0; i < 32 / kAtOnce; ++i) {
+                    const int q = row0 + i * kAtOnce + lane / kLanes, n = node_of(P, q);
+                    if (q < w.s.n_new * P.group)
+                        reinterpret_cast<uint4*>(static_cast<T*>(P.out.ptr) + (w.s.row0 + n) * P.out.token_stride +
+                                                 (int64_t)(head * P.group + q - n * P.group) * P.out.head_stride)[c] =
+                            *reinterpret_cast<const uint4*>(stage + piece(128, 32 * (wid & 3) + i * kAtOnce + lane / kLanes, c));
                 }
                 __syncwarp();
             }
-            if (is && fine) {
+            if (is) {
                 if (!whole) {
                     part[part_row] = top;
                     part[L::kRows + part_row] = sum;
@@ -416,94 +458,115 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         if (wid == 4 * kTiles) {
             // ------------------------------------------------ loads: of each unit the keys, then the values
             const int box = min(P.cache.page_tokens, kKeys), boxes = kKeys / box;
-            uint32_t n = 0, issued = 0;
+            uint32_t n = 0, slot = 0, parity = 1;  // loads made; the next one's slot, and the parity of its last release
             for (; w.more(); w.next(P, kKeys, L::kRows)) {
                 const int head = w.h / (w.items / P.cache.n_kv_heads);
+                const int32_t* table = P.page_table + (int64_t)w.b * P.table_stride;
+                auto page_of = [&](int u) {  // of this lane's box of unit u; -1: past the end, reads zeros
+                    const int key = u * kKeys + lane * box;
+                    return lane < boxes && key < w.s.len ? __ldg(table + (key >> P.page_log2)) : -1;
+                };
+                int page = page_of(w.u);
                 for (; w.u < w.end; ++w.u) {
-                    const int key = w.u * kKeys + lane * box;
-                    int page = -1;  // past the end: reads zeros
-                    if (lane < boxes && key < w.s.len) page = __ldg(P.page_table + (int64_t)w.b * P.table_stride + (key >> P.page_log2));
-                    for (int v = 0; v < 2; ++v, ++n) {
-                        const uint32_t slot = n % kSlots, at = ring + slot * L::kSlot + lane * box * 128;
-                        if (n >= kSlots) wait_warp(empty + 8 * slot, (n / kSlots + 1) & 1);
+                    const int next_page = w.u + 1 < w.end ? page_of(w.u + 1) : -1;
+                    const int y = (w.u * kKeys + lane * box) & (P.cache.page_tokens - 1);
+#pragma unroll
+                    for (int v = 0; v < 2; ++v) {
+                        const uint32_t bar = full + 8 * slot, at = ring + slot * L::kSlot + lane * box * 128;
+                        if (n >= kSlots) wait(empty + 8 * slot, parity);
+                        fine = __all_sync(~0u, fine);
                         if (!fine) continue;
-                        if (lane == 0) bar_expect(full + 8 * slot, L::kSlot);
+                        if (lane == 0) bar_expect(bar, L::kSlot);
                         __syncwarp();
                         if (lane < boxes) {
-                            const int y = key & (P.cache.page_tokens - 1);
 #pragma unroll
-                            for (int i = 0; i < D / 64; ++i)
-                                tma_load(at + i * kKeys * 128, v ? &map_v : &map_k, full + 8 * slot, 64 * i, y, head, page);
+                            for (int i = 0; i < D / 64; ++i) tma_load(at + i * kKeys * 128, v ? &map_v : &map_k, bar, 64 * i, y, head, page);
                         }
-                        issued = n + 1;
+                        ++n;
+                        if (++slot == kSlots) {
+                            slot = 0;
+                            parity ^= 1;
+                        }
                     }
+                    page = next_page;
                 }
             }
+            const uint32_t issued = n;
             // every load issued has landed before the block leaves (bounded again where a wait has run out)
             for (uint32_t i = issued > kSlots ? issued - kSlots : 0; i < issued; ++i) bar_wait(full + 8 * (i % kSlots), (i / kSlots) & 1);
-        } else if (wid == 4 * kTiles + 1) {
-            // ------------------------------------------------ products, issued by one thread
-            if (lane == 0) {
+        } else {
+            // ------------------------------------------------ products: a warp a tile, so that no tile's wait delays the other
+            const int t = wid - 4 * kTiles - 1;
+            if (t < kTiles) {
                 constexpr uint32_t kScores = instruction<T>(false, kKeys), kValues = instruction<T>(true, D);
-                uint32_t n = 0, items[2] = {0, 0}, units[2] = {0, 0};  // ring slots used; a tile's items and units begun
-                auto scores = [&](int t, uint32_t slot, int region) {
-                    const uint32_t q = base + t * 128 * D * 2, k = ring + slot * L::kSlot;
+                const uint32_t tm = uniform(tmem), q = uniform(operand(base + t * 128 * D * 2, 16)), o = uniform(tmem + L::kO + t * D);
+                struct Slot {  // of the ring: keys and values alternate
+                    uint32_t at, parity;
+                    __device__ __forceinline__ void next()
+                    {
+                        at += 2;
+                        if (at >= kSlots) {
+                            at -= kSlots;
+                            parity ^= 1;
+                        }
+                    }
+                } ks = {0, 0}, vs = {1, 0};
+                uint32_t items = 0, units = 0;  // of the tile, begun
+                auto scores = [&](int region) {
+                    const uint32_t k = uniform(operand(ring + ks.at * L::kSlot, 16)), d = uniform(tm + region * kKeys);
 #pragma unroll
                     for (int i = 0; i < D / 16; ++i)
-                        mma_shared(tmem + region * kKeys, operand(q + (i >> 2) * 128 * 128 + (i & 3) * 32, 16),
-                                   operand(k + (i >> 2) * kKeys * 128 + (i & 3) * 32, 16), kScores, i > 0);
+                        mma_shared(d, q + (((i >> 2) * 128 * 128 + (i & 3) * 32) >> 4), k + (((i >> 2) * kKeys * 128 + (i & 3) * 32) >> 4), kScores,
+                                   i > 0);
                     mma_commit(s_full + 8 * region);
-                };
-                auto values = [&](int t, uint32_t slot, int region, bool add) {
-                    const uint32_t v = ring + slot * L::kSlot;
-#pragma unroll
-                    for (int i = 0; i < kKeys / 16; ++i)
-                        mma_tensor(tmem + L::kO + t * D, tmem + region * kKeys + 8 * i, operand(v + i * 2048, kKeys * 128), kValues, add || i > 0);
-                    mma_commit(o_full + 8 * t);
+                    mma_commit(empty + 8 * ks.at);
+                    ks.next();
                 };
                 for (; w.more(); w.next(P, kKeys, L::kRows)) {
-                    const int count = w.end - w.begin, tiles = tiles_of(w);
-                    for (int t = 0; t < tiles; ++t) wait_thread(q_full + 8 * t, items[t]++ & 1);
-                    if (!wait_thread(full + 8 * (n % kSlots), (n / kSlots) & 1)) continue;
-                    fence_after();
-                    for (int t = 0; t < tiles; ++t) scores(t, n % kSlots, region_of(t, units[t]));
-                    mma_commit(empty + 8 * (n % kSlots));
-                    for (int i = 0; i < count && fine; ++i, n += 2) {
-                        // the next unit's scores go ahead of this one's values where they have a region of their own (one
-                        // tile), else right behind each tile's values: the softmax of one tile runs beside the other's products
-                        const uint32_t next = n + 2, value_slot = (n + 1) % kSlots;
-                        const bool more = i + 1 < count;
-                        auto wait_next = [&]() {
-                            const bool ok = wait_thread(full + 8 * (next % kSlots), (next / kSlots) & 1);
-                            fence_after();
-                            return ok;
-                        };
-                        if (kTiles == 1 && more) {
-                            if (!wait_next()) break;
-                            scores(0, next % kSlots, region_of(0, units[0] + 1));
-                            mma_commit(empty + 8 * (next % kSlots));
-                        }
-#pragma unroll
-                        for (int t = 0; t < kTiles; ++t) {
-                            if (t >= tiles) break;
-                            if (!wait_thread(p_full + 8 * region_of(t, units[t]), parity_of(units[t]))) break;
-                            if (t == 0 && !wait_thread(full + 8 * value_slot, ((n + 1) / kSlots) & 1)) break;
-                            fence_after();
-                            values(t, value_slot, region_of(t, units[t]), i > 0);
-                            ++units[t];
-                            if (t == tiles - 1) mma_commit(empty + 8 * value_slot);
-                            if (kTiles > 1 && more) {
-                                if (t == 0 && !wait_next()) break;
-                                scores(t, next % kSlots, t);
-                                if (t == tiles - 1) mma_commit(empty + 8 * (next % kSlots));
+                    const int count = w.end - w.begin;
+                    if (t >= tiles_of(w)) {  // the slots go by, each as it fills
+                        for (int i = 0; i < count; ++i) {
+                            wait(full + 8 * ks.at, ks.parity);
+                            wait(full + 8 * vs.at, vs.parity);
+                            if (lane == 0) {
+                                bar_arrive(empty + 8 * ks.at);
+                                bar_arrive(empty + 8 * vs.at);
                             }
+                            ks.next();
+                            vs.next();
                         }
+                        continue;
+                    }
+                    wait(q_full + 8 * t, items++ & 1);
+                    wait(full + 8 * ks.at, ks.parity);
+                    __syncwarp();
+                    fence_after();
+                    scores(region_of(t, units));
+                    for (int i = 0; i < count; ++i, ++units) {
+                        const int region = region_of(t, units);
+                        const bool more = i + 1 < count;
+                        if (more) {  // the next unit's scores go ahead of this one's values
+                            wait(full + 8 * ks.at, ks.parity);
+                            __syncwarp();
+                            fence_after();
+                            scores(region_of(t, units + 1));
+                        }
+                        const uint32_t v = uniform(operand(ring + vs.at * L::kSlot, kKeys * 128)), p = uniform(tm + region * kKeys);
+                        wait(full + 8 * vs.at, vs.parity);
+                        wait(p_full + 8 * region, parity_of(units));
+                        __syncwarp();
+                        fence_after();
+#pragma unroll
+                        for (int j = 0; j < kKeys / 16; ++j) mma_tensor(o, p + 8 * j, v + (j * 2048 >> 4), kValues, j > 0 || i > 0);
+                        mma_commit(o_full + 8 * region);
+                        mma_commit(empty + 8 * vs.at);
+                        vs.next();
                     }
                 }
                 mma_commit(done);  // every product is done before the tensor memory is given back
                 bar_wait(done, 0);
+                __syncwarp();
             }
-            __syncwarp();
         }
     }
     __syncthreads();
@@ -526,7 +589,7 @@ cudaError_t launch(const AttentionParams& p, cudaStream_t stream)
     const int blocks = sm_count() * L::kBlocksPerSm;
     err = launch_dependent(kernel, dim3(blocks), dim3(L::kThreads), L::kBytes, 1, stream, k, v, p);
     if (err != cudaSuccess) return err;
-    return launch_merge(p, blocks, L::kRows, stream);
+    return launch_merge(p, blocks, L::kRows, true, stream);
 }
 
 template <typename T>

@@ -14,11 +14,13 @@ namespace {
 
 constexpr int kThreads = 128;
 
-// The items that several blocks worked on, a row at a time: its parts in the order of the blocks.  Where a row has few
-// parts each warp takes a row (kSplit = 1), else the block's warps take a fourth of one row's parts each.
-template <typename T, int D>
-struct MergedRow {
-    static constexpr int kPer = D / 32;
+// The items that several blocks worked on: the parts of a row in the order of the blocks, parts of largest score m, weight
+// sum l and output o joined as sum_i 2^(m_i - m) o_i over sum_i 2^(m_i - m) l_i.  A warp takes kAhead rows of up to
+// kFewParts, whose loads are in flight together; of more parts (few rows over a long axis) the block's warps take a
+// fourth of one row's each.
+template <int D>
+struct RowOfParts {
+    static constexpr int kPer = D / 32;  // dimensions of a lane
     float o[kPer], m, l;
 
     __device__ __forceinline__ void add(float pm, float pl, const float (&po)[kPer])
@@ -29,41 +31,36 @@ struct MergedRow {
         for (int j = 0; j < kPer; ++j) o[j] = o[j] * fa + (pm == -INFINITY ? 0.f : po[j] * fb);
         m = mn;
     }
-    // parts [from, to) of row r of the item that block `first` begins
-    __device__ __forceinline__ void gather(const AttentionParams& P, int blocks, int rows, int r, int first, int from, int to, int lane)
-    {
-        m = -INFINITY;
-        l = 0.f;
-#pragma unroll
-        for (int j = 0; j < kPer; ++j) o[j] = 0.f;
-#pragma unroll 4
-        for (int i = from; i < to; ++i) {
-            const float* part = part_of_item(P, blocks, rows, D, first + i, i == 0 ? 1 : 0);
-            float po[kPer];
-#pragma unroll
-            for (int j = 0; j < kPer; ++j) po[j] = part[2 * rows + (size_t)r * D + lane * kPer + j];
-            add(part[r], part[rows + r], po);
-        }
-    }
+    template <typename T>
     __device__ __forceinline__ void write(const AttentionParams& P, const Seq& s, const SplitSlot& d, int r, int lane) const
     {
         const int node = node_of(P, d.row0 + r);
         const int64_t row = s.row0 + node, h = d.h * P.group + d.row0 + r - node * P.group;
         T* out = static_cast<T*>(P.out.ptr) + row * P.out.token_stride + h * P.out.head_stride + lane * kPer;
         const float inv = l > 0.f ? 1.f / l : 0.f;
-        uint32_t v[kPer / 2];
-#pragma unroll
-        for (int j = 0; j < kPer / 2; ++j) v[j] = Pair<T>::join(o[2 * j] * inv, o[2 * j + 1] * inv);
-#pragma unroll
-        for (int j = 0; j < kPer / 2; ++j) reinterpret_cast<uint32_t*>(out)[j] = v[j];
+        if (kPer == 4)
+            *reinterpret_cast<uint2*>(out) = make_uint2(Pair<T>::join(o[0] * inv, o[1] * inv), Pair<T>::join(o[kPer - 2] * inv, o[kPer - 1] * inv));
+        else
+            *reinterpret_cast<uint32_t*>(out) = Pair<T>::join(o[0] * inv, o[1] * inv);
         if (lane == 0 && P.lse) P.lse[row * P.n_q_heads + h] = l > 0.f ? (m + log2f(l)) * 0x1.62e43p-1f : -INFINITY;
     }
 };
+template <int kPer>
+__device__ __forceinline__ void load_part(const float* from, float (&o)[kPer])
+{
+    if constexpr (kPer == 4) {
+        const float4 v = *reinterpret_cast<const float4*>(from);
+        o[0] = v.x, o[1] = v.y, o[2] = v.z, o[3] = v.w;
+    } else {
+        const float2 v = *reinterpret_cast<const float2*>(from);
+        o[0] = v.x, o[1] = v.y;
+    }
+}
 
-constexpr int kFewParts = 8;
+constexpr int kAhead = 4, kFewParts = 8;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P, int blocks, int rows)
+__global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P, int blocks, int rows, int row_step, int lane_step)
 {
     constexpr int kPer = D / 32, kWarps = kThreads / 32;
     __shared__ float sm_o[kWarps][D], sm_m[kWarps], sm_l[kWarps];
@@ -73,17 +70,64 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P
     const Seq s = seq_of(P, d.b);
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, first = blockIdx.x, n = d.last - first + 1;
     const int end = min(rows, s.n_new * P.group - d.row0);
-    MergedRow<T, D> a;
+    auto part_at = [&](int i) { return part_of_item(P, blocks, rows, D, first + i, i == 0 ? 1 : 0); };
     if (n <= kFewParts) {
-        for (int r = blockIdx.y * kWarps + wid; r < end; r += gridDim.y * kWarps) {
-            a.gather(P, blocks, rows, r, first, 0, n, lane);
-            a.write(P, s, d, r, lane);
+        for (int r0 = (blockIdx.y * kWarps + wid) * kAhead; r0 < end; r0 += gridDim.y * kWarps * kAhead) {
+            RowOfParts<D> a[kAhead];
+            float factor[kAhead];  // of part `lane`
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                const bool is = lane < n && r0 + q < end;
+                a[q].m = is ? part_at(lane)[r0 + q] : -INFINITY;
+                a[q].l = is ? part_at(lane)[rows + r0 + q] : 0.f;
+            }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q) {
+                const float mine = a[q].m;
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) a[q].m = fmaxf(a[q].m, __shfl_xor_sync(~0u, a[q].m, off));
+                factor[q] = mine == -INFINITY ? 0.f : exp2_fast(mine - a[q].m);
+                a[q].l *= factor[q];
+#pragma unroll
+                for (int off = 16; off > 0; off >>= 1) a[q].l += __shfl_xor_sync(~0u, a[q].l, off);
+#pragma unroll
+                for (int j = 0; j < kPer; ++j) a[q].o[j] = 0.f;
+            }
+#pragma unroll 4
+            for (int i = 0; i < n; ++i) {
+                float po[kAhead][kPer];
+                const float* from = part_at(i) + 2 * rows + r0 * row_step + lane * lane_step;
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q)
+                    if (r0 + q < end) load_part<kPer>(from + q * row_step, po[q]);
+#pragma unroll
+                for (int q = 0; q < kAhead; ++q) {
+                    const float f = __shfl_sync(~0u, factor[q], i);
+                    if (r0 + q < end && f > 0.f)
+#pragma unroll
+                        for (int j = 0; j < kPer; ++j) a[q].o[j] += f * po[q][j];
+                }
+            }
+#pragma unroll
+            for (int q = 0; q < kAhead; ++q)
+                if (r0 + q < end) a[q].template write<T>(P, s, d, r0 + q, lane);
         }
         return;
     }
     const int per = (n + kWarps - 1) / kWarps;
     for (int r = blockIdx.y; r < end; r += gridDim.y) {
-        a.gather(P, blocks, rows, r, first, min(wid * per, n), min((wid + 1) * per, n), lane);
+        RowOfParts<D> a;
+        a.m = -INFINITY;
+        a.l = 0.f;
+#pragma unroll
+        for (int j = 0; j < kPer; ++j) a.o[j] = 0.f;
+        float po[kPer];
+#pragma unroll 4
+        for (int i = min(wid * per, n); i < min((wid + 1) * per, n); ++i) {
+            const float* part = part_at(i);
+            load_part<kPer>(part + 2 * rows + r * row_step + lane * lane_step, po);
+            a.add(part[r], part[rows + r], po);
+        }
 #pragma unroll
         for (int j = 0; j < kPer; ++j) sm_o[wid][lane * kPer + j] = a.o[j];
         sm_m[wid] = a.m;
@@ -92,12 +136,11 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P
         if (wid == 0) {
 #pragma unroll
             for (int w = 1; w < kWarps; ++w) {
-                float po[kPer];
 #pragma unroll
                 for (int j = 0; j < kPer; ++j) po[j] = sm_o[w][lane * kPer + j];
                 a.add(sm_m[w], sm_l[w], po);
             }
-            a.write(P, s, d, r, lane);
+            a.template write<T>(P, s, d, r, lane);
         }
         __syncthreads();
     }
@@ -150,14 +193,19 @@ cudaError_t make_cache_maps(const AttentionParams& p, int box_tokens, CUtensorMa
     return cudaSuccess;
 }
 
-cudaError_t launch_merge(const AttentionParams& p, int blocks, int rows, cudaStream_t stream)
+cudaError_t launch_merge(const AttentionParams& p, int blocks, int rows, bool columns, cudaStream_t stream)
 {
     const int most = p.group * p.max_nodes < rows ? p.group * p.max_nodes : rows;
-    const dim3 grid((unsigned)blocks, (unsigned)(most < 32 ? most : 32));
+    const int per_block = kThreads / 32 * kAhead;
+    const int y = (most + per_block - 1) / per_block, few = most < 8 ? most : 8;
+    const dim3 grid((unsigned)blocks, (unsigned)(y > few ? y : few));
     const bool bf = p.cache.dtype == CTR_BF16, wide = p.cache.head_dim == 128;
     auto kernel = bf ? (wide ? merge_kernel<__nv_bfloat16, 128> : merge_kernel<__nv_bfloat16, 64>)
                      : (wide ? merge_kernel<__half, 128> : merge_kernel<__half, 64>);
-    return launch_dependent(kernel, grid, dim3(kThreads), 0, 1, stream, p, blocks, rows);
+    // a lane's dimensions: four of 128, two of 64
+    const int per = p.cache.head_dim / 32;
+    return launch_dependent(kernel, grid, dim3(kThreads), 0, 1, stream, p, blocks, rows, columns ? per : p.cache.head_dim,
+                            columns ? per * rows : per);
 }
 
 size_t attention_workspace(const ctr_kv_cache& cache, int32_t n_q_heads, int32_t, int32_t max_nodes)
