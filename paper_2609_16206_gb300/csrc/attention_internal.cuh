@@ -246,7 +246,7 @@ struct Walk {
 // Workspace: blocks SplitSlots, then per block and slot the partial sums of up to `rows` rows: their maxima and
 // weight sums, and `rows` x head_dim fp32 outputs, row by row, or (columns) the rows of each head_dim / 32 dimensions
 // together, as a kernel with a row a thread writes them.
-__host__ __device__ __forceinline__ size_t slots_bytes(int blocks) { return ((size_t)blocks * sizeof(SplitSlot) + 255) / 256 * 256; }
+__host__ __device__ __forceinline__ size_t slots_bytes(int blocks) { return ((size_t)blocks * sizeof(SplitSlot) + 511) / 256 * 256; }
 __host__ __device__ __forceinline__ size_t part_floats(int rows, int d) { return (size_t)rows * (d + 2); }
 __device__ __forceinline__ SplitSlot* split_slots(const AttentionParams& P) { return reinterpret_cast<SplitSlot*>(P.ws); }
 __device__ __forceinline__ float* part_of_item(const AttentionParams& P, int blocks, int rows, int d, int block, int slot)

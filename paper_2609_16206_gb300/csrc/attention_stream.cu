@@ -420,7 +420,8 @@ cudaError_t launch(const AttentionParams& p, cudaStream_t stream)
     using L = Layout<D, kTiles>;
     constexpr int bytes = L::kBytes;
     auto kernel = stream_kernel<T, D, kTiles>;
-    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+    static std::atomic<uint64_t> devices{0};
+    err = allow_shared(kernel, bytes, devices);
     if (err != cudaSuccess) return err;
     const int blocks = sm_count() * L::kBlocksPerSm;
     err = launch_dependent(kernel, dim3(blocks), dim3(kThreads), bytes, 1, stream, k, v, p);

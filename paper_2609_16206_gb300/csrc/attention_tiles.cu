@@ -584,7 +584,8 @@ cudaError_t launch(const AttentionParams& p, cudaStream_t stream)
     cudaError_t err = make_cache_maps(p, p.cache.page_tokens < L::kKeys ? p.cache.page_tokens : L::kKeys, &k, &v);
     if (err != cudaSuccess) return err;
     auto kernel = tiles_kernel<T, D, kTiles>;
-    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, L::kBytes);
+    static std::atomic<uint64_t> devices{0};
+    err = allow_shared(kernel, L::kBytes, devices);
     if (err != cudaSuccess) return err;
     const int blocks = sm_count() * L::kBlocksPerSm;
     err = launch_dependent(kernel, dim3(blocks), dim3(L::kThreads), L::kBytes, 1, stream, k, v, p);

@@ -3,7 +3,9 @@
 // the ABI.
 #pragma once
 
+#include <atomic>
 #include <cstdint>
+#include <cstring>
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_runtime.h>
@@ -36,6 +38,20 @@ cudaError_t launch_dependent(void (*kernel)(KArgs...), dim3 grid, dim3 block, si
     cfg.attrs = attr;
     const cudaError_t err = cudaLaunchKernelEx(&cfg, kernel, args...);
     return err != cudaSuccess ? err : cudaGetLastError();
+}
+
+// More dynamic shared memory than 48 KB for a kernel, asked for once on each device: `most` for all of its launches.
+template <typename Kernel>
+cudaError_t allow_shared(Kernel* kernel, int most, std::atomic<uint64_t>& devices)
+{
+    int dev = 0;
+    cudaError_t err = cudaGetDevice(&dev);
+    if (err != cudaSuccess) return err;
+    const uint64_t bit = 1ull << (dev & 63);
+    if (dev < 64 && (devices.load(std::memory_order_acquire) & bit)) return cudaSuccess;
+    err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, most);
+    if (err == cudaSuccess) devices.fetch_or(bit, std::memory_order_release);
+    return err;
 }
 
 __device__ __forceinline__ void wait_for_previous_kernels()

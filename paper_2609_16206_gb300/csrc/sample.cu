@@ -955,7 +955,8 @@ template <typename T, int kThreads>
 cudaError_t launch_as(const SampleParams& p, int blocks, size_t bytes, cudaStream_t stream)
 {
     auto kernel = sample_kernel<T, kThreads>;
-    cudaError_t err = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
+    static std::atomic<uint64_t> devices{0};
+    const cudaError_t err = allow_shared(kernel, (CTR_MAX_VOCAB / kMaxCluster + 8) * (int)sizeof(T), devices);
     if (err != cudaSuccess) return err;
     return launch_dependent(kernel, dim3((unsigned)(p.n_rows * blocks)), dim3(kThreads), bytes, blocks, stream, p);
 }

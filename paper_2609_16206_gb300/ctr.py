@@ -353,7 +353,7 @@ class KvCache:
         if not (k.is_cuda and v.is_cuda):
             raise ValueError("expected a CUDA tensor")
         self.k, self.v = k, v
-        self.dtype, self.device = k.dtype, k.device
+        self.dtype, self.device, self.index = k.dtype, k.device, k.device.index
         self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k.shape
         self.struct = CtrKvCache(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], self.n_kv_heads, self.head_dim,
                                  self.page_tokens, self.n_pages, k.stride(0), k.stride(1), k.stride(2))
@@ -375,31 +375,43 @@ class Rope:
 
 def _rows(t, cache, name):
     """[tokens, heads, head_dim] in the cache's dtype, the last dimension contiguous."""
-    if t.dim() != 3 or t.dtype != cache.dtype or t.shape[2] != cache.head_dim or not t.is_cuda or \
-            (t.stride(2) != 1 and t.numel() > 0):
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or t.dtype is not cache.dtype or shape[2] != cache.head_dim or not t.is_cuda or \
+            (stride[2] != 1 and t.numel() > 0):
         raise ValueError(f"{name} must be a CUDA tensor [tokens, heads, {cache.head_dim}] of {cache.dtype}, the last "
                          "dimension contiguous")
-    return CtrRows(t.data_ptr(), t.stride(0), t.stride(1))
+    return CtrRows(t.data_ptr(), stride[0], stride[1])
 
 
 def _vector(t, dtype, n, name):
     if t is None:
         return None
-    if t.dtype != dtype or t.numel() != n:
-        raise ValueError(f"{name} must hold {n} elements of {dtype}")
-    return _ptr(t)
+    if t.dtype is not dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous CUDA tensor of {n} elements of {dtype}")
+    return t.data_ptr()
+
+
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # absent without CUDA
+
+
+def _stream_on(stream, index):
+    """The given stream's handle, or the current one's of device `index`."""
+    return _raw_stream(index) if stream is None else stream.cuda_stream
 
 
 def ctr_kv_append(cache: KvCache, rope: Rope, q, k, v, positions, slots, q_out, stream=None):
     """Rotate q into q_out, append the rotated k and v to their slots.  q, k, v: [tokens, heads, head_dim]; positions
     and slots: int64 per token (slot < 0: padding)."""
-    n = k.shape[0]
-    if k.shape != v.shape or k.dim() != 3 or k.shape[1] != cache.n_kv_heads or q.shape != q_out.shape or q.shape[0] != n:
+    k_shape, q_shape = k.shape, q.shape
+    n = k_shape[0]
+    if k_shape != v.shape or len(k_shape) != 3 or k_shape[1] != cache.n_kv_heads or q_shape != q_out.shape or q_shape[0] != n:
         raise ValueError("q, k, v and q_out must be [tokens, heads, head_dim] with the cache's heads")
-    _check("ctr_kv_append", lib().ctr_kv_append(
+    rc = (_lib or lib()).ctr_kv_append(
         cache.ref, rope.ref, _rows(q, cache, "q"), _rows(k, cache, "k"), _rows(v, cache, "v"),
-        _rows(q_out, cache, "q_out"), n, q.shape[1], _vector(positions, torch.int64, n, "positions"),
-        _vector(slots, torch.int64, n, "slots"), _stream(stream)))
+        _rows(q_out, cache, "q_out"), n, q_shape[1], _vector(positions, torch.int64, n, "positions"),
+        _vector(slots, torch.int64, n, "slots"), _stream_on(stream, cache.index))
+    if rc:
+        raise CtrError("ctr_kv_append", rc)
 
 
 def attention_workspace(cache: KvCache, n_q_heads: int, n_seqs: int, max_nodes: int) -> torch.Tensor:
@@ -414,28 +426,33 @@ def ctr_tree_attention(cache: KvCache, q, q_start, kv_len, page_table, out, work
     """Attention of the new tokens (rows of q, sequence b's from q_start[b] to q_start[b + 1]) over the cache that holds
     them.  q, out: [rows, heads, head_dim]; q_start int32 [n_seqs + 1]; kv_len int32 [n_seqs]; page_table int32
     [n_seqs, width]; tree_mask int64 [rows] (bit j: attends to new token j; None: a chain); lse fp32 [rows, heads]."""
-    rows, heads = q.shape[0], q.shape[1]
-    n_seqs = kv_len.numel()
-    if out.shape != q.shape or page_table.dim() != 2 or page_table.shape[0] != n_seqs or page_table.dtype != torch.int32:
+    q_shape, table_shape = q.shape, page_table.shape
+    rows, heads, n_seqs = q_shape[0], q_shape[1], kv_len.numel()
+    if out.shape != q_shape or len(table_shape) != 2 or table_shape[0] != n_seqs:
         raise ValueError("out must have q's shape, page_table must be int32 [n_seqs, width]")
-    _check("ctr_tree_attention", lib().ctr_tree_attention(
-        cache.ref, _rows(q, cache, "q"), _rows(out, cache, "out"), rows, heads, n_seqs, int(max_nodes),
+    rc = (_lib or lib()).ctr_tree_attention(
+        cache.ref, _rows(q, cache, "q"), _rows(out, cache, "out"), rows, heads, n_seqs, max_nodes,
         _vector(q_start, torch.int32, n_seqs + 1, "q_start"), _vector(kv_len, torch.int32, n_seqs, "kv_len"),
-        _ptr(page_table), page_table.shape[1], _vector(tree_mask, torch.int64, rows, "tree_mask"),
-        float(cache.head_dim ** -0.5 if scale is None else scale), _vector(lse, torch.float32, rows * heads, "lse"),
-        _vector(status, torch.int32, 1, "status"), _ptr(workspace), workspace.numel() * workspace.element_size(),
-        _stream(stream)))
+        _vector(page_table, torch.int32, n_seqs * table_shape[1], "page_table"), table_shape[1],
+        _vector(tree_mask, torch.int64, rows, "tree_mask"), cache.head_dim ** -0.5 if scale is None else scale,
+        _vector(lse, torch.float32, rows * heads, "lse"), _vector(status, torch.int32, 1, "status"), _ptr(workspace),
+        workspace.nbytes, _stream_on(stream, cache.index))
+    if rc:
+        raise CtrError("ctr_tree_attention", rc)
 
 
 def ctr_sample(logits, temperature, u, token, top_k=None, top_p=None, min_p=None, logprob=None, n_kept=None, stream=None):
     """A token per row of logits [rows, vocab] (bfloat16, float16 or float32, rows of any stride).  Per row: temperature,
     u in [0, 1), top_p and min_p fp32; top_k, token and n_kept int32; logprob fp32."""
-    if logits.dim() != 2 or logits.dtype not in _DTYPES or not logits.is_cuda or (logits.stride(1) != 1 and logits.shape[1] > 1):
+    shape, stride, dtype = logits.shape, logits.stride(), _DTYPES.get(logits.dtype)
+    if len(shape) != 2 or dtype is None or not logits.is_cuda or (stride[1] != 1 and shape[1] > 1):
         raise ValueError("logits must be a CUDA tensor [rows, vocab] of a floating type, the last dimension contiguous")
-    n, vocab = logits.shape
+    n, vocab = shape
     f32, i32 = torch.float32, torch.int32
-    _check("ctr_sample", lib().ctr_sample(
-        logits.data_ptr(), _DTYPES[logits.dtype], logits.stride(0) if n > 1 else vocab, n, vocab,
+    rc = (_lib or lib()).ctr_sample(
+        logits.data_ptr(), dtype, stride[0] if n > 1 else vocab, n, vocab,
         _vector(temperature, f32, n, "temperature"), _vector(top_k, i32, n, "top_k"), _vector(top_p, f32, n, "top_p"),
         _vector(min_p, f32, n, "min_p"), _vector(u, f32, n, "u"), _vector(token, i32, n, "token"),
-        _vector(logprob, f32, n, "logprob"), _vector(n_kept, i32, n, "n_kept"), _stream(stream)))
+        _vector(logprob, f32, n, "logprob"), _vector(n_kept, i32, n, "n_kept"), _stream_on(stream, logits.device.index))
+    if rc:
+        raise CtrError("ctr_sample", rc)
