@@ -1,17 +1,32 @@
-"""One decode step of a served model on this GPU: helpers around the operators of ``include/ctr_decode.h``.
+"""A decode instance on this GPU, and the calibration of the simulated one from it.
 
-``rope_turns`` makes the frequency words of ``ctr.Rope``.
+The simulator prices a decode step as ``dec_base + dec_per_seq n + KV / kv_div`` with constants that sec. III-B of the
+paper fits on the serving engine.  ``DecodeInstance`` is the part of an engine that those constants come from: a
+transformer of random weights whose attention runs on a paged KV cache with the operators of ``include/ctr_decode.h``
+(``ctr.ctr_kv_append``, ``ctr.ctr_tree_attention``, ``ctr.ctr_sample``); its projections are library products.
+``calibrate`` times its step over batch sizes and resident tokens and fits the constants, ``calibrated_sim`` puts them
+into a simulated cluster and the router's constants::
+
+    inst = decode.DecodeInstance(decode.ModelSpec(), max_seqs=64, kv_tokens=65_536)
+    fit = decode.calibrate(inst)
+    sim_cfg, consts = decode.calibrated_sim(fit)
 """
 from __future__ import annotations
 
+import dataclasses
 import math
+from dataclasses import dataclass
 
 import torch
+
+from . import ctr
+from . import workloads as W
 
 
 def rope_turns(rot_dim: int, base: float = 10000.0, factor: float = 1.0, trained_len: int = 0, fast: float = 32.0,
                slow: float = 1.0, device="cuda") -> torch.Tensor:
-    """The frequency word of every rotated pair: base^(-2i / rot_dim) / 2 pi turns per position, times 2^64.
+    """The frequency word of every rotated pair for ``ctr.Rope``: base^(-2i / rot_dim) / 2 pi turns per position, times
+    2^64.
 
     ``factor`` > 1 scales the positions for contexts longer than the model was trained on: with ``trained_len`` = 0
     every frequency is divided by it (linear interpolation); otherwise a pair that makes at least ``fast`` turns over
@@ -28,3 +43,224 @@ def rope_turns(rot_dim: int, base: float = 10000.0, factor: float = 1.0, trained
         w = int(f * (keep + (1 - keep) / factor) * 2.0 ** 64)
         words.append(w - (1 << 64) if w >= 1 << 63 else w)
     return torch.tensor(words, dtype=torch.int64, device=device)
+
+
+def tree_words(parents) -> list:
+    """A draft tree's attention words: node i attends to itself and its ancestors (parents[i] < i, -1 for a child of the
+    context).  As signed 64-bit integers, for an int64 tensor."""
+    words = []
+    for i, p in enumerate(parents):
+        if i >= ctr.CTR_MAX_NODES or not -1 <= p < i:
+            raise ValueError(f"at most {ctr.CTR_MAX_NODES} nodes, each after its parent")
+        words.append((words[p] if p >= 0 else 0) | 1 << i)
+    return [w - (1 << 64) if w >= 1 << 63 else w for w in words]
+
+
+def tree_depths(parents) -> list:
+    """Each node's distance from the context's last token, less one: its position is the context's length plus it."""
+    depths = []
+    for p in parents:
+        depths.append(depths[p] + 1 if p >= 0 else 0)
+    return depths
+
+
+@dataclass(frozen=True)
+class ModelSpec:
+    layers: int = 4
+    hidden: int = 1024
+    heads: int = 16
+    kv_heads: int = 2
+    head_dim: int = 128
+    ffn: int = 2816
+    vocab: int = 32_000
+    page_tokens: int = 16
+    dtype: torch.dtype = torch.bfloat16
+    rope_base: float = 1_000_000.0
+
+
+def _norm(x):
+    f = x.float()
+    return (f * torch.rsqrt(f.square().mean(-1, keepdim=True) + 1e-6)).to(x.dtype)
+
+
+class DecodeInstance:
+    """A transformer of random weights with a paged KV cache of ``kv_tokens`` tokens a layer for up to ``max_seqs``
+    sequences, which bring up to ``max_nodes`` tokens each in a step."""
+
+    def __init__(self, spec: ModelSpec, max_seqs: int, kv_tokens: int, max_nodes: int = 1, device="cuda", seed: int = 0):
+        self.spec, self.max_seqs, self.max_nodes, self.device = spec, max_seqs, max_nodes, device
+        g = torch.Generator(device=device).manual_seed(seed)
+
+        def weight(*shape):
+            return (torch.randn(*shape, device=device, generator=g) * shape[0] ** -0.5).to(spec.dtype)
+        qkv = (spec.heads + 2 * spec.kv_heads) * spec.head_dim
+        self.embed = torch.randn(spec.vocab, spec.hidden, device=device, generator=g).to(spec.dtype)
+        self.head = weight(spec.hidden, spec.vocab)
+        self.layers = [dict(qkv=weight(spec.hidden, qkv), out=weight(spec.heads * spec.head_dim, spec.hidden),
+                            up=weight(spec.hidden, 2 * spec.ffn), down=weight(spec.ffn, spec.hidden))
+                       for _ in range(spec.layers)]
+        self.pages = -(-kv_tokens // spec.page_tokens) + max_seqs
+        shape = (self.pages, spec.kv_heads, spec.page_tokens, spec.head_dim)
+        self.caches = [ctr.KvCache(torch.zeros(shape, device=device, dtype=spec.dtype),
+                                   torch.zeros(shape, device=device, dtype=spec.dtype)) for _ in range(spec.layers)]
+        self.rope = ctr.Rope(rope_turns(spec.head_dim, spec.rope_base, device=device))
+        self.workspace = ctr.attention_workspace(self.caches[0], spec.heads, max_seqs, max_nodes)
+        self.reset([])
+
+    def reset(self, lens):
+        """Begin with sequences of these lengths (their cache as it is); pages are dealt out in turn."""
+        if len(lens) > self.max_seqs:
+            raise ValueError(f"at most {self.max_seqs} sequences")
+        page, room = self.spec.page_tokens, self.max_nodes + 1
+        need = [-(-(n + room) // page) for n in lens]
+        if sum(need) > self.pages:
+            raise ValueError("the sequences do not fit the cache")
+        self.lens = list(lens)
+        rows = [[] for _ in lens]
+        free = iter(range(self.pages))
+        for j in range(max(need, default=0)):
+            for row, n in zip(rows, need):
+                if j < n:
+                    row.append(next(free))
+        self.width = max(need, default=1)
+        self.rows, self.free = rows, list(free)
+        self._upload()
+
+    def _upload(self):
+        table = [r + [0] * (self.width - len(r)) for r in self.rows]
+        self.table = torch.tensor(table, dtype=torch.int32, device=self.device).reshape(len(self.rows), self.width)
+
+    def grow(self, accepted):
+        """Each sequence keeps so many of its last step's tokens (its first ones)."""
+        page = self.spec.page_tokens
+        for b, n in enumerate(accepted):
+            self.lens[b] += int(n)
+            while len(self.rows[b]) * page < self.lens[b] + self.max_nodes:
+                self.rows[b].append(self.free.pop())
+        self.width = max(len(r) for r in self.rows)
+        self._upload()
+
+    def plan(self, parents=None):
+        """The step's index tensors: ``parents[b]`` is the draft tree of sequence b (None: one token each)."""
+        page = self.spec.page_tokens
+        parents = parents if parents is not None else [[-1]] * len(self.lens)
+        start, slots, positions, words, kv_len = [0], [], [], [], []
+        for n, row, tree in zip(self.lens, self.rows, parents):
+            if len(tree) > self.max_nodes:
+                raise ValueError(f"at most {self.max_nodes} tokens a sequence")
+            start.append(start[-1] + len(tree))
+            at = range(n, n + len(tree))
+            slots += [row[i // page] * page + i % page for i in at]
+            positions += [n + d for d in tree_depths(tree)]
+            words += tree_words(tree)
+            kv_len.append(n + len(tree))
+
+        def tensor(v, dt):
+            return torch.tensor(v, dtype=dt, device=self.device)
+        return dict(q_start=tensor(start, torch.int32), kv_len=tensor(kv_len, torch.int32), slots=tensor(slots, torch.int64),
+                    positions=tensor(positions, torch.int64), tree_mask=tensor(words, torch.int64))
+
+    def step(self, tokens, plan):
+        """Logits [tokens, vocab] of one step: every token's keys and values are in the cache afterwards."""
+        s = self.spec
+        x = self.embed[tokens]
+        n = x.shape[0]
+        a, b = s.heads, s.heads + s.kv_heads
+        for layer, cache in zip(self.layers, self.caches):
+            qkv = (_norm(x) @ layer["qkv"]).view(n, -1, s.head_dim)
+            q = qkv[:, :a]
+            ctr.ctr_kv_append(cache, self.rope, q, qkv[:, a:b], qkv[:, b:], plan["positions"], plan["slots"], q)
+            o = torch.empty(n, s.heads, s.head_dim, device=x.device, dtype=x.dtype)
+            ctr.ctr_tree_attention(cache, q, plan["q_start"], plan["kv_len"], self.table, o, self.workspace,
+                                   max_nodes=self.max_nodes, tree_mask=plan["tree_mask"])
+            x = x + o.view(n, -1) @ layer["out"]
+            up, gate = (_norm(x) @ layer["up"]).chunk(2, -1)
+            x = x + (up * torch.nn.functional.silu(gate)) @ layer["down"]
+        return _norm(x) @ self.head
+
+    def sample(self, logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+        """A token a row of logits, one setting for all rows."""
+        n = logits.shape[0]
+
+        def full(v, dt=torch.float32):
+            return torch.full((n,), v, dtype=dt, device=logits.device)
+        token = torch.empty(n, dtype=torch.int32, device=logits.device)
+        ctr.ctr_sample(logits, full(temperature), u, token, top_k=full(top_k, torch.int32), top_p=full(top_p),
+                       min_p=full(min_p))
+        return token
+
+
+@dataclass(frozen=True)
+class StepFit:
+    """dec_base_us + dec_us_per_seq n + KV / dec_kv_tokens_per_us, and the measured (n, KV, us) it was fitted to."""
+    dec_base_us: float
+    dec_us_per_seq: float
+    dec_kv_tokens_per_us: float
+    points: tuple
+
+    def step_us(self, n, kv):
+        return self.dec_base_us + self.dec_us_per_seq * n + kv / self.dec_kv_tokens_per_us
+
+
+def fit_steps(points) -> StepFit:
+    """Least squares of the step's three terms over (n, KV tokens, us) points, each point weighted by 1 / us (the fit is
+    of relative errors); terms that come out negative are held at 0 (the KV term: at 2^31 tokens a us)."""
+    a = torch.tensor([[1.0 / t, n / t, kv / t] for n, kv, t in points], dtype=torch.float64)
+    use = [0, 1, 2]
+    while True:
+        x = torch.linalg.lstsq(a[:, use], torch.ones(len(points), 1, dtype=torch.float64)).solution[:, 0].tolist()
+        keep = [c for c, v in zip(use, x) if v > 0]
+        if keep == use or not keep:
+            break
+        use = keep
+    c = dict(zip(use, x))
+    slope = max(c.get(2, 0.0), 2.0 ** -31)
+    return StepFit(max(c.get(0, 0.0), 0.0), max(c.get(1, 0.0), 0.0), 1.0 / slope, tuple(points))
+
+
+def time_step(inst: DecodeInstance, n: int, context: int, reps: int = 10) -> float:
+    """Microseconds of a decode step (one token a sequence, top-p sampling) of n sequences of ``context`` tokens, as a
+    captured graph on inst's device."""
+    inst.reset([context] * n)
+    plan = inst.plan()
+    tokens = torch.zeros(n, dtype=torch.int64, device=inst.device)
+    u = torch.full((n,), 0.5, device=inst.device)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(2):
+            inst.sample(inst.step(tokens, plan), u, top_p=0.95)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        inst.sample(inst.step(tokens, plan), u, top_p=0.95)
+    for _ in range(3):
+        graph.replay()
+    begin, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+    begin.record()
+    for _ in range(reps):
+        graph.replay()
+    end.record()
+    end.synchronize()
+    return begin.elapsed_time(end) * 1e3 / reps
+
+
+def calibrate(inst: DecodeInstance, batches=(1, 8, 32, 64), contexts=(64, 512, 2048), reps: int = 10) -> StepFit:
+    """The decode constants of this instance on this GPU, from the steps of the grid that fit its cache."""
+    room = (inst.pages - inst.max_seqs) * inst.spec.page_tokens
+    points = []
+    for n in batches:
+        for c in contexts:
+            if n <= inst.max_seqs and n * (c + inst.max_nodes + inst.spec.page_tokens) <= room:
+                points.append((n, n * c, time_step(inst, n, c, reps)))
+    if len(points) < 3:
+        raise ValueError("the cache holds fewer than three points of the grid")
+    return fit_steps(points)
+
+
+def calibrated_sim(fit: StepFit, sim: W.SimCfg = W.SimCfg(), consts: W.CostConsts = W.CALIBRATED):
+    """A simulated cluster whose decode instances step as measured, and the router's constants to match it: tau_dec is
+    the step of a single sequence, as in the presets.  The simulator's constants are whole microseconds."""
+    cfg = dataclasses.replace(sim, dec_base_us=max(1, round(fit.dec_base_us)), dec_us_per_seq=round(fit.dec_us_per_seq),
+                              dec_kv_tokens_per_us=max(1, min(1 << 31, round(fit.dec_kv_tokens_per_us))))
+    return cfg, consts.replace(tau_dec_us=max(1, round(fit.dec_base_us + fit.dec_us_per_seq)))
