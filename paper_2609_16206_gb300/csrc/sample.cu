@@ -30,7 +30,7 @@ namespace {
 constexpr int kMaxCluster = 8;
 constexpr int kList = 256;          // tokens that the first block ranks
 constexpr int kGather = 512;        // candidates of the cluster, an equal share of them to a block
-constexpr int kUnits = 25;          // bins of y: (-1, 0] .. (-16, -15], then twos to -34, below which no weight is left
+constexpr int kUnits = 25;          // bins of y: units around 0 .. -15, then pairs of them down to around -33; no weight is lower
 constexpr int kShared = 7;          // the first of them, of few tokens, are the block's; of the others each thread has its own,
                                     // where its at most 255 weights below 2^24 have a sum below 2^32
 constexpr int kPieces = 4;          // of a block's part of the row, each a bulk copy
@@ -68,8 +68,8 @@ __device__ __forceinline__ void exponents(const Scale& s, float x0, float x1, fl
 
 // round(2^31 2^y): y = k + f with k its nearest integer (by adding 1.5 2^23 + 32, whose low bits are then k + 32), 2^f =
 // 1 + f (c1 + f (c2 + ...)), a minimax fit on [-1/2, 1/2] with constant term 1: relative error 9.2e-8 before
-// rounding and 1.9e-7 with every fp32 step rounded.  Half of it is computed, which rounds alike.
-__device__ __forceinline__ void weights(const Scale& s, float y0, float y1, uint32_t& w0, uint32_t& w1)
+// rounding and 1.9e-7 with every fp32 step rounded.  Half of it is computed, which rounds alike.  u: -k.
+__device__ __forceinline__ void weights(const Scale& s, float y0, float y1, uint32_t& w0, uint32_t& w1, int& u0, int& u1)
 {
     constexpr float kMagic = 0x1.8p+23f + 32.f;
     const uint64_t y = pack(y0, y1);
@@ -83,6 +83,14 @@ __device__ __forceinline__ void weights(const Scale& s, float y0, float y1, uint
     p = add2(fma2(p, f, s.mz), pack(0.5f, 0.5f));
     w0 = __float2uint_rn(__uint_as_float((uint32_t)p + ((uint32_t)t << 23)));
     w1 = __float2uint_rn(__uint_as_float((uint32_t)(p >> 32) + ((uint32_t)(t >> 32) << 23)));
+    const uint32_t zero = __float_as_uint(kMagic);
+    u0 = (int)(zero - (uint32_t)t);
+    u1 = (int)(zero - (uint32_t)(t >> 32));
+}
+__device__ __forceinline__ void weights(const Scale& s, float y0, float y1, uint32_t& w0, uint32_t& w1)
+{
+    int u0, u1;
+    weights(s, y0, y1, w0, w1, u0, u1);
 }
 __device__ __forceinline__ uint32_t weight_of(const Scale& s, float x)
 {
@@ -469,11 +477,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     };
 
     // ---- bins of y: masses (or counts) of units, then of a unit's kBins parts
-    auto unit_of = [](float y) {
-        const int u = (int)-y;
-        return u < 16 ? u : min(8 + (u >> 1), kUnits - 1);
-    };
-    auto unit_begin = [](int u) { return (float)(u < 16 ? u : 2 * u - 16); };  // -y there
+    auto unit_at = [](int u) { return u < 16 ? u : min(8 + (u >> 1), kUnits - 1); };  // u: -y rounded to an integer
+    auto unit_of = [&](float y) { return unit_at(__float2int_rn(-y)); };
+    auto unit_begin = [](int u) { return (float)(u < 16 ? u : 2 * u - 16) - 0.5f; };  // -y there
     auto unit_width = [](int u) { return u < 16 ? 1.f : 2.f; };
     auto clear_units = [&] {
 #pragma unroll
@@ -485,16 +491,19 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         if (unit >= kShared) sm.own_bins[unit - kShared][tid] += w;
         else atomicAdd(reinterpret_cast<unsigned long long*>(&sm.unit_bins[unit]), (unsigned long long)w);
     };
-    // the block's units, then the cluster's: to every block, in peers' order
+    // the block's units; the barrier of the cluster that follows gives them to the others
     auto join_units = [&] {
         __syncthreads();
         for (int u = kShared + wid; u < kUnits; u += kWarps) {
             uint64_t m = 0;
-            for (int i = lane; i < kThreads; i += 32) m += sm.own_bins[u - kShared][i];
+#pragma unroll
+            for (int i = 0; i < kThreads; i += 32) m += sm.own_bins[u - kShared][i + lane];
 #pragma unroll
             for (int off = 16; off > 0; off >>= 1) m += __shfl_xor_sync(~0u, m, off);
             if (lane == 0) sm.unit_bins[u] = m;
         }
+    };
+    auto cluster_barrier = [&] {
         if (blocks > 1) cluster_sync();
         else __syncthreads();
     };
@@ -514,9 +523,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         over = __shfl_sync(~0u, upto - m, max(unit, 0));
         return unit;
     };
-    // the part of a unit that y lies in: below 0 or from kBins on where it lies above or below the unit
-    auto part_index = [&](float y, int unit) { return (int)floorf((-y - unit_begin(unit)) * ((float)kBins / unit_width(unit))); };
-    // the same over the parts of a unit, on top of `over`; a barrier of the cluster stands before
+    // the part of its unit that y lies in
+    auto part_index = [&](float y, int unit) { return max(0, min((int)((-y - unit_begin(unit)) * ((float)kBins / unit_width(unit))), kBins - 1)); };
+    // The same over the parts of a unit, on top of `over`; a barrier of the cluster stands before, and another has to
+    // follow before the bins' memory is written again.
     auto find_part = [&](bool by_mass, uint64_t goal, uint64_t& over) {
         uint64_t m = 0;  // of part `tid`
         for (uint32_t b = 0; b < blocks; ++b) {
@@ -538,8 +548,7 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             sm.found[0] = tid;
             sm.found[1] = upto - m;
         }
-        if (blocks > 1) cluster_sync();  // no block writes over its bins while another reads them
-        else __syncthreads();
+        __syncthreads();
         over = sm.found[1];
         return (int)sm.found[0];
     };
@@ -547,7 +556,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     // ---- the cut: logits above cut_value, and those equal to it up to cut_index
     constexpr float kLowest = -3.402823466e38f;  // of the finite ones: others are in no cut
     // a logit below every one whose y is above -units (the rounding of y is 2^-22 of it)
-    auto below_units = [&](float units) { return fmaxf(s.top - (units * 1.00001f + 1e-5f) / s.rate - fabsf(s.top) * 1e-5f, kLowest); };
+    const float rate = fmaxf(s.rate, 1e-38f);
+    auto below_units = [&](float units) { return fmaxf(s.top - (units * 1.00001f + 1e-5f) / rate - fabsf(s.top) * 1e-5f, kLowest); };
+    auto above_units = [&](float units) { return s.top - fmaxf(units * 0.99999f - 1e-5f, 0.f) / rate + fabsf(s.top) * 1e-5f; };  // and above
     const float weightless = below_units(34.f);   // from it on down
     float cut_value = weightless;
     int cut_index = P.vocab;
@@ -558,22 +569,30 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         for (int i = tid; i < 2 * kBins; i += kThreads) (&sm.bins[0][0])[i] = 0;
         __syncthreads();
         floor = fmaxf(floor, below_units(unit_begin(unit) + unit_width(unit)));
+        const float over = above_units(unit_begin(unit));
         Words v = {0, 0, 0};
         each_pair([&](float x0, float x1, int at) {
             if (!(fmaxf(x0, x1) >= floor)) return;
+            if (fminf(x0, x1) > over && fminf(x0, x1) > cut_value) {
+                v.n += 2;
+                return;
+            }
             float y[2];
             const float e[2] = {x0, x1};
+            uint32_t w[2];
+            int u[2];
             exponents(s, x0, x1, y[0], y[1]);
+            weights(s, y[0], y[1], w[0], w[1], u[0], u[1]);
 #pragma unroll
             for (int j = 0; j < 2; ++j) {
-                const int b = part_index(y[j], unit);
-                if (b >= kBins || !(e[j] >= floor) || !in_cut(e[j], at + j)) continue;
+                u[j] = unit_at(u[j]);
+                if (u[j] > unit || !(e[j] >= floor) || !in_cut(e[j], at + j)) continue;
                 ++v.n;
-                if (b < 0) continue;
+                if (u[j] < unit) continue;
+                const int b = part_index(y[j], unit);
                 v.high = max(v.high, ~key_of(e[j]));
-                const uint32_t w = by_mass ? weight_of(s, e[j]) : 1u;
-                atomicAdd(&sm.bins[0][b], w & 0xffffu);
-                if (by_mass) atomicAdd(&sm.bins[1][b], w >> 16);
+                atomicAdd(&sm.bins[0][b], by_mass ? w[j] & 0xffffu : 1u);
+                if (by_mass) atomicAdd(&sm.bins[1][b], w[j] >> 16);
             }
         });
         return exchange_words(v);
@@ -653,14 +672,15 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
     auto cut_in = [&](bool by_mass, uint64_t goal, uint64_t over, int unit, float floor) {
         const int from = find_part(by_mass, goal, over);
         floor = fmaxf(floor, below_units(unit_begin(unit) + (float)(from + 1) * (unit_width(unit) / kBins)));
+        const float ceiling = above_units(unit_begin(unit) + (float)from * (unit_width(unit) / kBins));
         // the part's largest and smallest key: in between are its tokens alone
         Words v = {0, 0, 0};
         each_pair([&](float x0, float x1, int at) {
-            if (!(fmaxf(x0, x1) >= floor)) return;
+            if (!(fmaxf(x0, x1) >= floor) || !(fminf(x0, x1) <= ceiling)) return;
             float y0, y1;
             exponents(s, x0, x1, y0, y1);
-            const bool in0 = part_index(y0, unit) == from && x0 >= floor && in_cut(x0, at);
-            const bool in1 = part_index(y1, unit) == from && x1 >= floor && in_cut(x1, at + 1);
+            const bool in0 = unit_of(y0) == unit && part_index(y0, unit) == from && x0 >= floor && in_cut(x0, at);
+            const bool in1 = unit_of(y1) == unit && part_index(y1, unit) == from && x1 >= floor && in_cut(x1, at + 1);
             if (in0) v = Words{max(v.top, key_of(x0)), max(v.high, ~key_of(x0)), 0};
             if (in1) v = Words{max(v.top, key_of(x1)), max(v.high, ~key_of(x1)), 0};
         });
@@ -710,8 +730,12 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         exchange(Sums{0, 0, 0, lane == 0 ? c : 0u}, &before);
         uint64_t seen = before.n;  // by the warps before this one
         for (int i = 0; i < wid; ++i) seen += sm.warp[i].n;
-        uint32_t index = 0;
-        if (seen < need && need <= seen + c) {  // in this warp's run: 32 logits at a time
+        // where this block's end: all of them, none, or as many as this warp finds
+        uint32_t block_seen = 0;
+        for (int i = 0; i < kWarps; ++i) block_seen += sm.warp[i].n;
+        if (tid == 0) sm.found[0] = need >= before.n + block_seen ? (uint64_t)P.vocab : ~0ull;
+        __syncthreads();
+        if (seen < need && need < seen + c) {  // 32 logits at a time
             for (int i = run0 * kN; i < run1 * kN; i += 32) {
                 const bool is = i + lane < run1 * kN && to_float(reinterpret_cast<const T*>(part)[i + lane]) == value && in_cut(value, base + i + lane);
                 uint32_t m = __ballot_sync(~0u, is);
@@ -720,11 +744,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     continue;
                 }
                 for (; seen + 1 < need; ++seen) m &= m - 1;
-                index = (uint32_t)(base + i + __ffs(m));  // one past it
+                if (lane == 0) sm.found[0] = (uint64_t)(base + i + __ffs(m) - 1);
                 break;
             }
+        } else if (seen < need && need == seen + c && lane == 0 && need < before.n + block_seen) {
+            sm.found[0] = (uint64_t)(base + run1 * kN - 1);  // up to this run's end
         }
-        cut_index = (int)exchange_words(Words{index, 0, 0}).top - 1;  // the goal is reached, so that there is one
+        __syncthreads();
+        cut_index = (int)(int64_t)sm.found[0];
         cut_value = value;
     };
     // the cut to the first tokens that reach the goal, among those from `floor` on; nothing where they do not
@@ -741,10 +768,9 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
             if (in1) add_to_unit(unit_of(y1), w1);
         });
         join_units();
+        cluster_barrier();
         uint64_t over = 0;
         const int unit = find_unit(goal, over);
-        if (blocks > 1) cluster_sync();
-        else __syncthreads();
         if (unit < 0) return;
         split_unit(by_mass, unit, floor);
         cut_in(by_mass, goal, over, unit, floor);
@@ -775,11 +801,14 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
         } else if (cut) {
             clear_units();
             each_pair([&](float x0, float x1, int) {
-                weigh(x0, x1, y0, y1, w0, w1);
+                int u0, u1;
+                exponents(s, x0, x1, y0, y1);
+                weights(s, y0, y1, w0, w1, u0, u1);
                 v.a += (uint64_t)w0 + w1;
-                add_to_unit(unit_of(y0), w0);
-                add_to_unit(unit_of(y1), w1);
+                add_to_unit(unit_at(u0), w0);
+                add_to_unit(unit_at(u1), w1);
             });
+            join_units();
         } else {
             each_pair([&](float x0, float x1, int) {
                 weigh(x0, x1, y0, y1, w0, w1);
@@ -806,11 +835,10 @@ __global__ void __launch_bounds__(kThreads, 1024 / kThreads) sample_kernel(const
                     if (unit_of(y0) <= last) add_to_unit(unit_of(y0), w0);
                     if (unit_of(y1) <= last) add_to_unit(unit_of(y1), w1);
                 });
+                join_units();
+                cluster_barrier();
             }
-            join_units();
             unit = find_unit(goal, over);
-            if (blocks > 1) cluster_sync();  // no block goes on to other bins while another reads these
-            else __syncthreads();
             const Words in = split_unit(true, unit, weightless);
             // few tokens up to the unit's end: no block has more than its share of the list
             by_list = in.n <= (uint32_t)min(kList, (int)(kGather / blocks));
