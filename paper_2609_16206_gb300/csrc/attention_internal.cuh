@@ -105,8 +105,11 @@ __device__ __forceinline__ float exp2_fast(float x)
 // or second slot of the workspace, and the merge kernel joins the slots of an item in the order of its blocks.
 constexpr int kUnitCost = 2, kItemCost = 1;
 
-struct SplitSlot {           // the item that a block begins and does not end
-    int32_t b, h, row0, last;  // sequence (-1: none), KV head, first row, the block that ends it
+struct __align__(16) SplitSlot {  // the item that a block begins and does not end
+    int32_t rows;              // of the item from row0 on (0: no such item)
+    int32_t row0, h, last;     // first row of the sequence's KV head, the head, the block that ends the item
+    int64_t first;             // the sequence's first row of q
+    int64_t reserved;
 };
 
 __device__ __forceinline__ int units_of(const Seq& s, int unit)
@@ -235,17 +238,24 @@ struct Walk {
         }
         enter(0);
     }
-    // the block that ends the item, which this range begins at cost `range_end - left`
-    __device__ __forceinline__ int last_block(const Range& r) const
+    // what the merge needs to know of an item that this range begins, at cost `range end - left`
+    __device__ __forceinline__ SplitSlot split(const AttentionParams& P, const Range& r, int head, int row0) const
     {
+        SplitSlot d;
         const int64_t pos = r.end - left + kItemCost + (int64_t)kUnitCost * units - 1;
-        return (int)(((pos + 1) * r.blocks - 1) / r.total);  // the largest c with floor(total c / blocks) <= pos
+        d.last = (int)(((pos + 1) * r.blocks - 1) / r.total);  // the largest c with floor(total c / blocks) <= pos
+        d.rows = s.n_new * P.group - row0;
+        d.row0 = row0;
+        d.h = head;
+        d.first = s.row0;
+        d.reserved = 0;
+        return d;
     }
 };
 
 // Workspace: blocks SplitSlots, then per block and slot the partial sums of up to `rows` rows: their maxima and
-// weight sums, and `rows` x head_dim fp32 outputs, row by row, or (columns) the rows of each head_dim / 32 dimensions
-// together, as a kernel with a row a thread writes them.
+// weight sums, and `rows` x head_dim fp32 outputs, row by row, or (columns) the rows of each four dimensions together,
+// as a kernel with a row a thread writes and reads them.
 __host__ __device__ __forceinline__ size_t slots_bytes(int blocks) { return ((size_t)blocks * sizeof(SplitSlot) + 511) / 256 * 256; }
 __host__ __device__ __forceinline__ size_t part_floats(int rows, int d) { return (size_t)rows * (d + 2); }
 __device__ __forceinline__ SplitSlot* split_slots(const AttentionParams& P) { return reinterpret_cast<SplitSlot*>(P.ws); }

@@ -100,7 +100,7 @@ stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
     wait_for_previous_kernels();
 
     const Range range = find_range<kThreads>(P, kUnit, L::kRows, blockIdx.x, gridDim.x, reinterpret_cast<int64_t*>(smem + L::kScratch));
-    if (tid == 0) split_slots(P)[blockIdx.x].b = -1;
+    if (tid == 0) split_slots(P)[blockIdx.x].rows = 0;
     if (range.end <= range.begin) return;
 
     Walk make, take;  // the chunks to load and the ones to compute on
@@ -399,14 +399,8 @@ stream_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__
                     }
                 }
             }
-        if (tid == 0 && take.begin == 0 && !whole) {  // the last item of the range: later blocks end it
-            SplitSlot d;
-            d.b = take.b;
-            d.h = take.h;
-            d.row0 = 0;
-            d.last = take.last_block(range);
-            split_slots(P)[blockIdx.x] = d;
-        }
+        // the last item of the range: later blocks end it
+        if (tid == 0 && take.begin == 0 && !whole) split_slots(P)[blockIdx.x] = take.split(P, range, take.h, 0);
         take.next(P, kUnit, L::kRows);
     }
 }

@@ -186,7 +186,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     }
     wait_for_previous_kernels();
     const Range range = find_range<L::kThreads>(P, kKeys, L::kRows, blockIdx.x, gridDim.x, reinterpret_cast<int64_t*>(smem + L::kScratch));
-    if (tid == 0) split_slots(P)[blockIdx.x].b = -1;
+    if (tid == 0) split_slots(P)[blockIdx.x].rows = 0;
     if (range.end <= range.begin) return;  // the whole block, before it holds any tensor memory
     if (wid == 0) {
         asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(base + L::kTmem), "r"((uint32_t)L::kColumns)
@@ -410,15 +410,9 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                         *reinterpret_cast<uint4*>(stage + piece(128, r, 4 * c + i)) = make_uint4(v[0], v[1], v[2], v[3]);
                     }
                 } else if (is) {
-                    constexpr int kPer = D / 32;  // dimensions of a lane of the merge
-                    float* to = part + 2 * L::kRows + (32 * c / kPer * L::kRows + part_row) * kPer;
+                    uint4* to = reinterpret_cast<uint4*>(part + 2 * L::kRows) + 8 * c * L::kRows + part_row;
 #pragma unroll
-                    for (int i = 0; i < 32 / kPer; ++i) {
-                        if constexpr (kPer == 4)
-                            *reinterpret_cast<uint4*>(to + i * L::kRows * kPer) = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
-                        else
-                            *reinterpret_cast<uint2*>(to + i * L::kRows * kPer) = make_uint2(x[2 * i], x[2 * i + 1]);
-                    }
+                    for (int i = 0; i < 8; ++i) to[i * L::kRows] = make_uint4(x[4 * i], x[4 * i + 1], x[4 * i + 2], x[4 * i + 3]);
                 }
             }
             if (whole) {  // the warp's rows, whole ones at a time
@@ -443,14 +437,8 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                     P.lse[at * P.n_q_heads + q_head] = sum > 0.f ? (top + log2f(sum)) * 0x1.62e43p-1f : -INFINITY;
                 }
             }
-            if (tid == 0 && w.begin == 0 && !whole) {  // the last item of the range: later blocks end it
-                SplitSlot d;
-                d.b = w.b;
-                d.h = head;
-                d.row0 = row;
-                d.last = w.last_block(range);
-                split_slots(P)[blockIdx.x] = d;
-            }
+            // the last item of the range: later blocks end it
+            if (tid == 0 && w.begin == 0 && !whole) split_slots(P)[blockIdx.x] = w.split(P, range, head, row);
             fence_before();
         }
     } else {

@@ -17,7 +17,7 @@ constexpr int kThreads = 128;
 // The items that several blocks worked on: the parts of a row in the order of the blocks, parts of largest score m, weight
 // sum l and output o joined as sum_i 2^(m_i - m) o_i over sum_i 2^(m_i - m) l_i.  A warp takes kAhead rows of up to
 // kFewParts, whose loads are in flight together; of more parts (few rows over a long axis) the block's warps take a
-// fourth of one row's each.
+// fourth of one row's each.  (For parts laid out row by row.)
 template <int D>
 struct RowOfParts {
     static constexpr int kPer = D / 32;  // dimensions of a lane
@@ -32,10 +32,10 @@ struct RowOfParts {
         m = mn;
     }
     template <typename T>
-    __device__ __forceinline__ void write(const AttentionParams& P, const Seq& s, const SplitSlot& d, int r, int lane) const
+    __device__ __forceinline__ void write(const AttentionParams& P, const SplitSlot& d, int r, int lane) const
     {
         const int node = node_of(P, d.row0 + r);
-        const int64_t row = s.row0 + node, h = d.h * P.group + d.row0 + r - node * P.group;
+        const int64_t row = d.first + node, h = d.h * P.group + d.row0 + r - node * P.group;
         T* out = static_cast<T*>(P.out.ptr) + row * P.out.token_stride + h * P.out.head_stride + lane * kPer;
         const float inv = l > 0.f ? 1.f / l : 0.f;
         if (kPer == 4)
@@ -60,16 +60,15 @@ __device__ __forceinline__ void load_part(const float* from, float (&o)[kPer])
 constexpr int kAhead = 4, kFewParts = 8;
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P, int blocks, int rows, int row_step, int lane_step)
+__global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P, int blocks, int rows)
 {
     constexpr int kPer = D / 32, kWarps = kThreads / 32;
     __shared__ float sm_o[kWarps][D], sm_m[kWarps], sm_l[kWarps];
     wait_for_previous_kernels();
     const SplitSlot d = split_slots(P)[blockIdx.x];
-    if (d.b < 0) return;
-    const Seq s = seq_of(P, d.b);
+    if (d.rows == 0) return;
     const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, first = blockIdx.x, n = d.last - first + 1;
-    const int end = min(rows, s.n_new * P.group - d.row0);
+    const int end = min(rows, d.rows);
     auto part_at = [&](int i) { return part_of_item(P, blocks, rows, D, first + i, i == 0 ? 1 : 0); };
     if (n <= kFewParts) {
         for (int r0 = (blockIdx.y * kWarps + wid) * kAhead; r0 < end; r0 += gridDim.y * kWarps * kAhead) {
@@ -96,10 +95,10 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P
 #pragma unroll 4
             for (int i = 0; i < n; ++i) {
                 float po[kAhead][kPer];
-                const float* from = part_at(i) + 2 * rows + r0 * row_step + lane * lane_step;
+                const float* from = part_at(i) + 2 * rows + r0 * D + lane * kPer;
 #pragma unroll
                 for (int q = 0; q < kAhead; ++q)
-                    if (r0 + q < end) load_part<kPer>(from + q * row_step, po[q]);
+                    if (r0 + q < end) load_part<kPer>(from + q * D, po[q]);
 #pragma unroll
                 for (int q = 0; q < kAhead; ++q) {
                     const float f = __shfl_sync(~0u, factor[q], i);
@@ -110,7 +109,7 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P
             }
 #pragma unroll
             for (int q = 0; q < kAhead; ++q)
-                if (r0 + q < end) a[q].template write<T>(P, s, d, r0 + q, lane);
+                if (r0 + q < end) a[q].template write<T>(P, d, r0 + q, lane);
         }
         return;
     }
@@ -125,7 +124,7 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P
 #pragma unroll 4
         for (int i = min(wid * per, n); i < min((wid + 1) * per, n); ++i) {
             const float* part = part_at(i);
-            load_part<kPer>(part + 2 * rows + r * row_step + lane * lane_step, po);
+            load_part<kPer>(part + 2 * rows + r * D + lane * kPer, po);
             a.add(part[r], part[rows + r], po);
         }
 #pragma unroll
@@ -140,10 +139,52 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P
                 for (int j = 0; j < kPer; ++j) po[j] = sm_o[w][lane * kPer + j];
                 a.add(sm_m[w], sm_l[w], po);
             }
-            a.template write<T>(P, s, d, r, lane);
+            a.template write<T>(P, d, r, lane);
         }
         __syncthreads();
     }
+}
+
+// The same of parts laid out by columns: a lane a row, a warp a fourth of the dimensions, eight of them at a time.
+template <typename T, int D>
+__global__ void __launch_bounds__(kThreads) merge_columns_kernel(const AttentionParams P, int blocks, int rows)
+{
+    wait_for_previous_kernels();
+    const SplitSlot d = split_slots(P)[blockIdx.x];
+    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, r = blockIdx.y * 32 + lane;
+    if (r >= min(rows, d.rows)) return;
+    const int first = blockIdx.x, n = d.last - first + 1;
+    auto part_at = [&](int i) { return part_of_item(P, blocks, rows, D, first + i, i == 0 ? 1 : 0); };
+    float m = -INFINITY, l = 0.f;
+    for (int i = 0; i < n; ++i) m = fmaxf(m, part_at(i)[r]);
+    float o[D / 4];
+#pragma unroll
+    for (int j = 0; j < D / 4; ++j) o[j] = 0.f;
+    for (int i = 0; i < n; ++i) {
+        const float* part = part_at(i);
+        const float pm = part[r], f = pm == -INFINITY ? 0.f : exp2_fast(pm - m);
+        l += f * part[rows + r];
+        const float4* from = reinterpret_cast<const float4*>(part + 2 * rows) + (size_t)wid * (D / 16) * rows + r;
+        float4 v[D / 16];
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) v[j] = f > 0.f ? from[j * rows] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int j = 0; j < D / 16; ++j) {
+            o[4 * j] += f * v[j].x;
+            o[4 * j + 1] += f * v[j].y;
+            o[4 * j + 2] += f * v[j].z;
+            o[4 * j + 3] += f * v[j].w;
+        }
+    }
+    const int node = node_of(P, d.row0 + r);
+    const int64_t row = d.first + node, h = d.h * P.group + d.row0 + r - node * P.group;
+    uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(P.out.ptr) + row * P.out.token_stride + h * P.out.head_stride + wid * (D / 4));
+    const float inv = l > 0.f ? 1.f / l : 0.f;
+#pragma unroll
+    for (int j = 0; j < D / 32; ++j)
+        out[j] = make_uint4(Pair<T>::join(o[8 * j] * inv, o[8 * j + 1] * inv), Pair<T>::join(o[8 * j + 2] * inv, o[8 * j + 3] * inv),
+                            Pair<T>::join(o[8 * j + 4] * inv, o[8 * j + 5] * inv), Pair<T>::join(o[8 * j + 6] * inv, o[8 * j + 7] * inv));
+    if (wid == 0 && P.lse) P.lse[row * P.n_q_heads + h] = l > 0.f ? (m + log2f(l)) * 0x1.62e43p-1f : -INFINITY;
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -196,16 +237,15 @@ cudaError_t make_cache_maps(const AttentionParams& p, int box_tokens, CUtensorMa
 cudaError_t launch_merge(const AttentionParams& p, int blocks, int rows, bool columns, cudaStream_t stream)
 {
     const int most = p.group * p.max_nodes < rows ? p.group * p.max_nodes : rows;
-    const int per_block = kThreads / 32 * kAhead;
-    const int y = (most + per_block - 1) / per_block, few = most < 8 ? most : 8;
-    const dim3 grid((unsigned)blocks, (unsigned)(y > few ? y : few));
     const bool bf = p.cache.dtype == CTR_BF16, wide = p.cache.head_dim == 128;
-    auto kernel = bf ? (wide ? merge_kernel<__nv_bfloat16, 128> : merge_kernel<__nv_bfloat16, 64>)
-                     : (wide ? merge_kernel<__half, 128> : merge_kernel<__half, 64>);
-    // a lane's dimensions: four of 128, two of 64
-    const int per = p.cache.head_dim / 32;
-    return launch_dependent(kernel, grid, dim3(kThreads), 0, 1, stream, p, blocks, rows, columns ? per : p.cache.head_dim,
-                            columns ? per * rows : per);
+    const int per_block = columns ? 32 : kThreads / 32 * kAhead, few = columns ? 1 : most < 8 ? most : 8;
+    const int y = (most + per_block - 1) / per_block;
+    auto by_rows = bf ? (wide ? merge_kernel<__nv_bfloat16, 128> : merge_kernel<__nv_bfloat16, 64>)
+                      : (wide ? merge_kernel<__half, 128> : merge_kernel<__half, 64>);
+    auto by_columns = bf ? (wide ? merge_columns_kernel<__nv_bfloat16, 128> : merge_columns_kernel<__nv_bfloat16, 64>)
+                         : (wide ? merge_columns_kernel<__half, 128> : merge_columns_kernel<__half, 64>);
+    return launch_dependent(columns ? by_columns : by_rows, dim3((unsigned)blocks, (unsigned)(y > few ? y : few)), dim3(kThreads), 0, 1, stream,
+                            p, blocks, rows);
 }
 
 size_t attention_workspace(const ctr_kv_cache& cache, int32_t n_q_heads, int32_t, int32_t max_nodes)
