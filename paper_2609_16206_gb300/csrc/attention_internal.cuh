@@ -98,12 +98,13 @@ __device__ __forceinline__ float exp2_fast(float x)
 
 // ---------------------------------------------------------------- the split of the work
 // A sequence's KV head is an item of ceil(len / unit) units, one at least, or several such items where its query rows
-// (group x new tokens) are more than the item_rows that a block takes.  Items cost kUnitCost a unit and kItemCost
-// for their begin and end, in half units of time; the cost of all items, in order, is cut into equal ranges, one a
-// block, and a cut inside an item goes to the unit that it falls in.  A range holds whole items and at most two parts
+// (group x new tokens) are more than the item_rows that a block takes.  An item costs a unit each and item_cost for its
+// begin and end; the cost of all items, in order, is cut into equal ranges, one a block, and a cut inside an item goes
+// to the unit that it falls in.  (Where the blocks have few units each, an item's begin and end are no longer a part of
+// a block's time but all of it, and only the units count.)  A range holds whole items and at most two parts
 // of items, its first and last; such a part leaves its sums in the block's first (an item begun by an earlier block)
 // or second slot of the workspace, and the merge kernel joins the slots of an item in the order of its blocks.
-constexpr int kUnitCost = 2, kItemCost = 1;
+constexpr int kFewUnits = 8;  // of a block
 
 struct __align__(16) SplitSlot {  // the item that a block begins and does not end
     int32_t rows;              // of the item from row0 on (0: no such item)
@@ -116,81 +117,88 @@ __device__ __forceinline__ int units_of(const Seq& s, int unit)
 {
     return s.n_new == 0 ? 0 : s.len <= unit ? 1 : (s.len + unit - 1) / unit;
 }
-__device__ __forceinline__ int64_t cost_of(int units) { return units == 0 ? 0 : (int64_t)kUnitCost * units + kItemCost; }
-// the unit of an item that a cut `off` into its cost falls in
-__device__ __forceinline__ int unit_at(int64_t off) { return off <= kItemCost ? 0 : (int)((off - kItemCost) / kUnitCost); }
-
-__device__ __forceinline__ int items_of(const AttentionParams& P, const Seq& s, int item_rows)
+// items of a KV head
+__device__ __forceinline__ int groups_of(const AttentionParams& P, const Seq& s, int item_rows)
 {
     const int rows = s.n_new * P.group;
-    return P.cache.n_kv_heads * (rows <= item_rows ? 1 : (rows + item_rows - 1) / item_rows);
+    return rows <= item_rows ? 1 : (rows + item_rows - 1) / item_rows;
 }
 
 struct Range {
     int64_t begin, end, total;  // of the cost
-    int blocks;                 // with work: each has a unit at least
-    int b;                      // the sequence that it begins in, and where in it (over its KV heads)
+    int item_cost, blocks;      // blocks with work: each has a unit at least
+    int b;                      // the sequence that it begins in, and where in it (over its items)
     int64_t within;
 };
 
-// The range of block c; by all threads of the block.  scratch: kThreads / 32 + 2 words of 64 bits.
+// The range of block c; by all threads of the block.  scratch: 2 * kThreads / 32 + 2 words of 64 bits.
 template <int kThreads>
-__device__ Range find_range(const AttentionParams& P, int unit, int item_rows, int c, int blocks, int64_t* scratch)
+__device__ Range find_range(const AttentionParams& P, int unit, int item_rows, int item_cost, int c, int blocks, int64_t* scratch)
 {
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
     const int per = (P.n_seqs + kThreads - 1) / kThreads;
     const int first = min(tid * per, P.n_seqs), last = min(first + per, P.n_seqs);
-    auto cost_at = [&](int b) {
+    int64_t my_items = 0, my_units = 0;
+    for (int b = first; b < last; ++b) {
         const Seq s = seq_of(P, b);
-        return cost_of(units_of(s, unit)) * items_of(P, s, item_rows);
-    };
-    int64_t mine = 0;
-    for (int b = first; b < last; ++b) mine += cost_at(b);
-    int64_t sum = mine;
+        const int units = units_of(s, unit), items = units > 0 ? P.cache.n_kv_heads * groups_of(P, s, item_rows) : 0;
+        my_items += items;
+        my_units += (int64_t)items * units;
+    }
+    int64_t items = my_items, units = my_units;  // of the threads up to this one
 #pragma unroll
     for (int off = 1; off < 32; off <<= 1) {
-        const int64_t v = __shfl_up_sync(~0u, sum, off);
-        if (lane >= off) sum += v;
+        const int64_t i = __shfl_up_sync(~0u, items, off), u = __shfl_up_sync(~0u, units, off);
+        if (lane >= off) items += i, units += u;
     }
-    if (lane == 31) scratch[wid] = sum;
+    if (lane == 31) {
+        scratch[2 * wid] = items;
+        scratch[2 * wid + 1] = units;
+    }
     __syncthreads();
-    Range r;
-    r.total = 0;
+    int64_t all_items = 0, all_units = 0;
 #pragma unroll
     for (int w = 0; w < kWarps; ++w) {
-        if (w == wid) sum += r.total;
-        r.total += scratch[w];
+        if (w == wid) items += all_items, units += all_units;
+        all_items += scratch[2 * w];
+        all_units += scratch[2 * w + 1];
     }
-    r.blocks = (int)min((int64_t)blocks, r.total / (kUnitCost + kItemCost));
+    Range r;
+    r.item_cost = all_units < (int64_t)kFewUnits * blocks ? 0 : item_cost;
+    r.total = all_units + r.item_cost * all_items;
+    r.blocks = (int)min((int64_t)blocks, r.total / (1 + r.item_cost));
     r.begin = r.end = r.within = 0;
     r.b = 0;
     if (c >= r.blocks) return r;  // the whole block
     r.begin = r.total * c / r.blocks;
     r.end = r.total * (c + 1) / r.blocks;
-    int64_t at = sum - mine;
-    if (at <= r.begin && r.begin < sum) {
+    int64_t at = units - my_units + r.item_cost * (items - my_items);
+    if (at <= r.begin && r.begin < units + r.item_cost * items) {
         for (int b = first; b < last; ++b) {
-            const int64_t n = cost_at(b);
+            const Seq s = seq_of(P, b);
+            const int u = units_of(s, unit);
+            const int64_t n = u == 0 ? 0 : (int64_t)(u + r.item_cost) * P.cache.n_kv_heads * groups_of(P, s, item_rows);
             if (r.begin < at + n) {
-                scratch[kWarps] = b;
-                scratch[kWarps + 1] = r.begin - at;
+                scratch[2 * kWarps] = b;
+                scratch[2 * kWarps + 1] = r.begin - at;
                 break;
             }
             at += n;
         }
     }
     __syncthreads();
-    r.b = (int)scratch[kWarps];
-    r.within = scratch[kWarps + 1];
+    r.b = (int)scratch[2 * kWarps];
+    r.within = scratch[2 * kWarps + 1];
     return r;
 }
 
-// A block's way through its range: the items in order (h: of the sequence) and of each the units [u, end).
+// A block's way through its range: the items in order (of a sequence's heads, their groups of rows) and of each the
+// units [u, end).
 struct Walk {
     Seq s;
-    int b, h, u, begin, end, units, items;
-    int64_t left;              // of the range's cost, from the item's begin on
+    int b, head, group, u, begin, end, units, groups, item_cost;
+    int64_t left;                 // of the range's cost, from the item's begin on
     int raw_lo, raw_hi, raw_len;  // the next sequence's bounds, loaded ahead
 
     __device__ __forceinline__ void load_ahead(const AttentionParams& P)
@@ -200,49 +208,55 @@ struct Walk {
         raw_hi = __ldg(P.q_start + n + 1);
         raw_len = __ldg(P.kv_len + n);
     }
+    // the unit of the item that a cut `off` into its cost falls in
+    __device__ __forceinline__ int unit_at(int64_t off) const { return off <= item_cost ? 0 : (int)min((int64_t)units, off - item_cost); }
     __device__ __forceinline__ void enter(int64_t off)
     {
         begin = u = unit_at(off);
-        end = min(units, unit_at(left));
+        end = unit_at(left);
     }
     __device__ __forceinline__ bool more() const { return left > 0 && end > 0; }
     __device__ __forceinline__ void start(const AttentionParams& P, const Range& r, int unit, int item_rows)
     {
         b = r.b;
         left = r.end - r.begin;
+        item_cost = r.item_cost;
         end = 0;
         if (left <= 0) return;
         s = seq_of(P, b);
         units = units_of(s, unit);
-        items = items_of(P, s, item_rows);
-        const int64_t cost = cost_of(units);
-        h = (int)(r.within / cost);
-        const int64_t off = r.within - h * cost;
+        groups = groups_of(P, s, item_rows);
+        const int64_t item = r.within / (units + item_cost), off = r.within - item * (units + item_cost);
+        head = (int)(item / groups);
+        group = (int)(item - (int64_t)head * groups);
         left += off;
         enter(off);
         load_ahead(P);
     }
     __device__ __forceinline__ void next(const AttentionParams& P, int unit, int item_rows)
     {
-        left -= cost_of(units);
+        left -= units + item_cost;
         if (left <= 0) return;
-        if (++h == items) {
-            h = 0;
-            do {
-                ++b;
-                s = seq_from(P, raw_lo, raw_hi, raw_len);
-                units = units_of(s, unit);
-                load_ahead(P);
-            } while (units == 0);
-            items = items_of(P, s, item_rows);
+        if (++group == groups) {
+            group = 0;
+            if (++head == P.cache.n_kv_heads) {
+                head = 0;
+                do {
+                    ++b;
+                    s = seq_from(P, raw_lo, raw_hi, raw_len);
+                    units = units_of(s, unit);
+                    load_ahead(P);
+                } while (units == 0);
+                groups = groups_of(P, s, item_rows);
+            }
         }
         enter(0);
     }
     // what the merge needs to know of an item that this range begins, at cost `range end - left`
-    __device__ __forceinline__ SplitSlot split(const AttentionParams& P, const Range& r, int head, int row0) const
+    __device__ __forceinline__ SplitSlot split(const AttentionParams& P, const Range& r, int row0) const
     {
         SplitSlot d;
-        const int64_t pos = r.end - left + kItemCost + (int64_t)kUnitCost * units - 1;
+        const int64_t pos = r.end - left + item_cost + units - 1;
         d.last = (int)(((pos + 1) * r.blocks - 1) / r.total);  // the largest c with floor(total c / blocks) <= pos
         d.rows = s.n_new * P.group - row0;
         d.row0 = row0;

@@ -35,6 +35,7 @@ struct Layout {
     // the softmax takes over: at launch 384 x 168, then 256 x 216 + 128 x 72, the same sum
     static constexpr int kThreads = kTiles == 1 ? 192 : 384;
     static constexpr int kBlocksPerSm = kTiles == 1 ? 2 : 1;
+    static constexpr int kItemCost = kTiles == 1 ? 4 : 6;      // measured: 12,000 cycles, of 2,900 and 1,900 a unit
     static constexpr int kSlot = kKeys * D * 2;                // bytes of a ring slot: a unit's keys or its values
     static constexpr int kQ = kRows * D * 2;
     static constexpr int kSlots = kTiles == 1 ? 5 : 10;
@@ -44,7 +45,7 @@ struct Layout {
     static constexpr int kBars = kRing + kSlots * kSlot;
     static constexpr int kNBars = 2 * kSlots + 15;
     static constexpr int kScratch = kBars + kNBars * 8;
-    static constexpr int kBad = kScratch + (kThreads / 32 + 2) * 8;  // two words of new tokens with values not finite
+    static constexpr int kBad = kScratch + (kThreads / 32 + 1) * 16;  // two words of new tokens with values not finite
     static constexpr int kTmem = kBad + 16;
     static constexpr int kBytes = kTmem + 16;
     static constexpr int kColumns = kTiles == 1 ? 256 : 512;   // of tensor memory: two regions of scores a tile, then outputs
@@ -185,7 +186,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         asm volatile("prefetch.tensormap [%0];" ::"l"(&map_v) : "memory");
     }
     wait_for_previous_kernels();
-    const Range range = find_range<L::kThreads>(P, kKeys, L::kRows, blockIdx.x, gridDim.x, reinterpret_cast<int64_t*>(smem + L::kScratch));
+    const Range range = find_range<L::kThreads>(P, kKeys, L::kRows, L::kItemCost, blockIdx.x, gridDim.x, reinterpret_cast<int64_t*>(smem + L::kScratch));
     if (tid == 0) split_slots(P)[blockIdx.x].rows = 0;
     if (range.end <= range.begin) return;  // the whole block, before it holds any tensor memory
     if (wid == 0) {
@@ -214,10 +215,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
     Walk w;
     w.start(P, range, kKeys, L::kRows);
     // an item's tiles with rows
-    auto tiles_of = [&](const Walk& at) {
-        const int groups = at.items / P.cache.n_kv_heads;
-        return kTiles == 1 || at.s.n_new * P.group - at.h % groups * L::kRows <= 128 ? 1 : 2;
-    };
+    auto tiles_of = [&](const Walk& at) { return kTiles == 1 || at.s.n_new * P.group - at.group * L::kRows <= 128 ? 1 : 2; };
     if (wid < 4 * kTiles) {
         if (kTiles == 2) asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
         // ------------------------------------------------ softmax: a row a thread
@@ -226,46 +224,50 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         const uint32_t o_at = tmem + lanes + L::kO + tile * D;
         const float scale = P.scale_log2 == 0.f ? 1.f : fabsf(P.scale_log2);
         uint32_t units = 0, block_units = 0, items = 0;  // of the tile; of the block; items of the block
-        for (; w.more(); w.next(P, kKeys, L::kRows), ++items) {
-            const int groups = w.items / P.cache.n_kv_heads, head = w.h / groups;
-            const int row = (w.h - head * groups) * L::kRows + tile * 128 + r;
+        // The warp's 32 queries, a row to D / 8 neighbouring lanes, copied from the item before's last scores on (from its
+        // end, where its outputs go through their place).
+        constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kLoads = 32 / kAtOnce;
+        auto row_of = [&](const Walk& at, int i) { return at.group * L::kRows + 32 * wid + i * kAtOnce + lane / kLanes; };
+        auto place_of = [&](int i) { return base + tile * 128 * D * 2 + piece(128, 32 * (wid & 3) + i * kAtOnce + lane / kLanes, lane % kLanes); };
+        auto copy_queries = [&](const Walk& at) {
+#pragma unroll 4
+            for (int i = 0; i < kLoads; ++i) {
+                const int q = row_of(at, i), n = node_of(P, q);
+                const bool there = q < at.s.n_new * P.group && P.scale_log2 != 0.f;
+                const T* src = static_cast<const T*>(P.q.ptr);
+                if (there) src += (at.s.row0 + n) * P.q.token_stride + (int64_t)(at.head * P.group + q - n * P.group) * P.q.head_stride + 8 * (lane % kLanes);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(place_of(i)), "l"(src), "r"(there ? 16 : 0) : "memory");
+            }
+        };
+        Walk ahead = w;
+        if (w.more()) copy_queries(w);
+        for (; w.more(); w = ahead, ++items) {
+            const int head = w.head, row = w.group * L::kRows + tile * 128 + r;
             const bool is = row < w.s.n_new * P.group;
             const int node = is ? node_of(P, row) : 0;
             const int64_t at = w.s.row0 + node, q_head = head * P.group + row - node * P.group;
             const uint64_t mask = !is ? 0 : P.tree_mask ? __ldg(reinterpret_cast<const unsigned long long*>(P.tree_mask) + at) : ~0ull >> (63 - node);
+            ahead.next(P, kKeys, L::kRows);
             // all rows begin an item together: no thread still reads the word of bad tokens that the next item takes
             asm volatile("bar.sync 1, %0;" ::"r"(128 * kTiles) : "memory");
             if (tid == 0) bad_tokens[(items + 1) & 1] = 0;
             if (tile >= tiles_of(w)) {
                 block_units += w.end - w.begin;
+                if (ahead.more()) copy_queries(ahead);
                 continue;
             }
-            {
-                // The warp's 32 queries, a row to D / 8 neighbouring lanes; the last scores of the item before are done.  A
-                // negative scale turns them round, a scale of 0 is a query of zeros: the factor that the maxima and
-                // exponents take is positive.
-                constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
-                const uint32_t turn = P.scale_log2 < 0.f ? 0x80008000u : 0u;
-                const int row0 = (w.h - head * groups) * L::kRows + 32 * wid, c = lane % kLanes;
-#pragma unroll
-                for (int i = 0; i < 32 / kAtOnce; i += 8) {
-                    uint4 v[8];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        const int q = row0 + (i + j) * kAtOnce + lane / kLanes, n = node_of(P, q);
-                        const T* src = static_cast<const T*>(P.q.ptr) + (w.s.row0 + n) * P.q.token_stride + (int64_t)(head * P.group + q - n * P.group) * P.q.head_stride;
-                        v[j] = q < w.s.n_new * P.group && P.scale_log2 != 0.f ? __ldg(reinterpret_cast<const uint4*>(src) + c) : make_uint4(0, 0, 0, 0);
-                    }
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        v[j].x ^= turn, v[j].y ^= turn, v[j].z ^= turn, v[j].w ^= turn;
-                        *reinterpret_cast<uint4*>(smem + tile * 128 * D * 2 + piece(128, 32 * (wid & 3) + (i + j) * kAtOnce + lane / kLanes, c)) = v[j];
-                    }
+            asm volatile("cp.async.wait_all;" ::: "memory");
+            if (P.scale_log2 < 0.f) {  // queries turned round: the factor that the maxima and exponents take is positive (0: they are zeros)
+#pragma unroll 1
+                for (int i = 0; i < kLoads; ++i) {
+                    uint4* v = reinterpret_cast<uint4*>(smem + (place_of(i) - base));
+                    v->x ^= 0x80008000u, v->y ^= 0x80008000u, v->z ^= 0x80008000u, v->w ^= 0x80008000u;
                 }
-                fence_async();
-                __syncwarp();
-                if (lane == 0) bar_arrive(q_full + 8 * tile);
             }
+            fence_async();
+            __syncwarp();
+            if (lane == 0) bar_arrive(q_full + 8 * tile);
+            const bool whole = w.begin == 0 && w.end == w.units;
             float top = -INFINITY, sum = 0.f;  // top: what the exponents are relative to, 2^-kLift of the largest
             for (; w.u < w.end; ++w.u, ++units, ++block_units) {
                 const int key = w.u * kKeys;
@@ -276,6 +278,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 wait(s_full + 8 * region, parity_of(units));
                 __syncwarp();
                 fence_after();
+                if (w.u + 1 == w.end && !whole && ahead.more()) copy_queries(ahead);
 #pragma unroll
                 for (int c = 0; c < kKeys / 64; ++c) {
                     uint32_t x[64];
@@ -378,7 +381,6 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             wait(o_full + 8 * region_of(tile, units - 1), parity_of(units - 1));
             __syncwarp();
             fence_after();
-            const bool whole = w.begin == 0 && w.end == w.units;
             const float inv = whole ? (sum > 0.f ? 1.f / sum : 0.f) : 1.f;
             const uint64_t bad = is && fine ? bad_tokens[items & 1] & mask : 0;
             float* part = part_of_item(P, gridDim.x, L::kRows, D, blockIdx.x, w.begin == 0 ? 1 : 0);
@@ -417,17 +419,17 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             }
             if (whole) {  // the warp's rows, whole ones at a time
                 __syncwarp();
-                constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes;
-                const int row0 = (w.h - head * groups) * L::kRows + 32 * wid, c = lane % kLanes;
+                const int c = lane % kLanes;
 #pragma unroll 4
-                for (int i = 0; i < 32 / kAtOnce; ++i) {
-                    const int q = row0 + i * kAtOnce + lane / kLanes, n = node_of(P, q);
+                for (int i = 0; i < kLoads; ++i) {
+                    const int q = row_of(w, i), n = node_of(P, q);
                     if (q < w.s.n_new * P.group)
                         reinterpret_cast<uint4*>(static_cast<T*>(P.out.ptr) + (w.s.row0 + n) * P.out.token_stride +
                                                  (int64_t)(head * P.group + q - n * P.group) * P.out.head_stride)[c] =
                             *reinterpret_cast<const uint4*>(stage + piece(128, 32 * (wid & 3) + i * kAtOnce + lane / kLanes, c));
                 }
                 __syncwarp();
+                if (ahead.more()) copy_queries(ahead);
             }
             if (is) {
                 if (!whole) {
@@ -438,7 +440,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
                 }
             }
             // the last item of the range: later blocks end it
-            if (tid == 0 && w.begin == 0 && !whole) split_slots(P)[blockIdx.x] = w.split(P, range, head, row);
+            if (tid == 0 && w.begin == 0 && !whole) split_slots(P)[blockIdx.x] = w.split(P, range, row);
             fence_before();
         }
     } else {
@@ -448,7 +450,7 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             const int box = min(P.cache.page_tokens, kKeys), boxes = kKeys / box;
             uint32_t n = 0, slot = 0, parity = 1;  // loads made; the next one's slot, and the parity of its last release
             for (; w.more(); w.next(P, kKeys, L::kRows)) {
-                const int head = w.h / (w.items / P.cache.n_kv_heads);
+                const int head = w.head;
                 const int32_t* table = P.page_table + (int64_t)w.b * P.table_stride;
                 auto page_of = [&](int u) {  // of this lane's box of unit u; -1: past the end, reads zeros
                     const int key = u * kKeys + lane * box;
