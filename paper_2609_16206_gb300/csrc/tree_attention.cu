@@ -145,46 +145,67 @@ __global__ void __launch_bounds__(kThreads) merge_kernel(const AttentionParams P
     }
 }
 
-// The same of parts laid out by columns: a lane a row, a warp a fourth of the dimensions, eight of them at a time.
+// The same of parts laid out by columns: a lane a row, 16 dimensions a warp, two parts in flight together, with what they
+// are scaled by.  Narrow warps, and no load that waits for another: the time is the loads' latency (32 trees of 16 nodes,
+// 20 MB of parts: 5 us, and 12 with a warp's 32 dimensions loaded part by part behind their maxima).
+constexpr int kColumns = 16, kTogether = 2;
+
 template <typename T, int D>
 __global__ void __launch_bounds__(kThreads) merge_columns_kernel(const AttentionParams P, int blocks, int rows)
 {
+    constexpr int kPer = kColumns / 4;
     wait_for_previous_kernels();
     const SplitSlot d = split_slots(P)[blockIdx.x];
-    const int lane = threadIdx.x & 31, wid = threadIdx.x >> 5, r = blockIdx.y * 32 + lane;
+    const int lane = threadIdx.x & 31, r = blockIdx.y * 32 + lane, column = (blockIdx.z * (kThreads / 32) + (threadIdx.x >> 5)) * kColumns;
     if (r >= min(rows, d.rows)) return;
-    const int first = blockIdx.x, n = d.last - first + 1;
-    auto part_at = [&](int i) { return part_of_item(P, blocks, rows, D, first + i, i == 0 ? 1 : 0); };
-    float m = -INFINITY, l = 0.f;
-    for (int i = 0; i < n; ++i) m = fmaxf(m, part_at(i)[r]);
-    float o[D / 4];
+    const int n = d.last - (int)blockIdx.x + 1;
+    float o[kColumns], m = -INFINITY, l = 0.f;
 #pragma unroll
-    for (int j = 0; j < D / 4; ++j) o[j] = 0.f;
-    for (int i = 0; i < n; ++i) {
-        const float* part = part_at(i);
-        const float pm = part[r], f = pm == -INFINITY ? 0.f : exp2_fast(pm - m);
-        l += f * part[rows + r];
-        const float4* from = reinterpret_cast<const float4*>(part + 2 * rows) + (size_t)wid * (D / 16) * rows + r;
-        float4 v[D / 16];
+    for (int j = 0; j < kColumns; ++j) o[j] = 0.f;
+    for (int i = 0; i < n; i += kTogether) {
+        float pm[kTogether], pl[kTogether];
+        float4 v[kTogether][kPer];
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) v[j] = f > 0.f ? from[j * rows] : make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int k = 0; k < kTogether; ++k) {
+            const bool is = i + k < n;
+            const float* part = part_of_item(P, blocks, rows, D, blockIdx.x + i + k, i + k == 0 ? 1 : 0);
+            const float4* from = reinterpret_cast<const float4*>(part + 2 * rows) + (size_t)(column / 4) * rows + r;
+            pm[k] = is ? part[r] : -INFINITY;
+            pl[k] = is ? part[rows + r] : 0.f;
 #pragma unroll
-        for (int j = 0; j < D / 16; ++j) {
-            o[4 * j] += f * v[j].x;
-            o[4 * j + 1] += f * v[j].y;
-            o[4 * j + 2] += f * v[j].z;
-            o[4 * j + 3] += f * v[j].w;
+            for (int j = 0; j < kPer; ++j) v[k][j] = is ? from[j * rows] : make_float4(0.f, 0.f, 0.f, 0.f);
+        }
+        float high = m;
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) high = fmaxf(high, pm[k]);
+        const float fix = m == -INFINITY ? 0.f : exp2_fast(m - high);
+        m = high;
+        l *= fix;
+#pragma unroll
+        for (int j = 0; j < kColumns; ++j) o[j] *= fix;
+#pragma unroll
+        for (int k = 0; k < kTogether; ++k) {
+            if (pm[k] == -INFINITY) continue;
+            const float f = exp2_fast(pm[k] - m);
+            l += f * pl[k];
+#pragma unroll
+            for (int j = 0; j < kPer; ++j) {
+                o[4 * j] += f * v[k][j].x;
+                o[4 * j + 1] += f * v[k][j].y;
+                o[4 * j + 2] += f * v[k][j].z;
+                o[4 * j + 3] += f * v[k][j].w;
+            }
         }
     }
     const int node = node_of(P, d.row0 + r);
     const int64_t row = d.first + node, h = d.h * P.group + d.row0 + r - node * P.group;
-    uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(P.out.ptr) + row * P.out.token_stride + h * P.out.head_stride + wid * (D / 4));
+    uint4* out = reinterpret_cast<uint4*>(static_cast<T*>(P.out.ptr) + row * P.out.token_stride + h * P.out.head_stride + column);
     const float inv = l > 0.f ? 1.f / l : 0.f;
 #pragma unroll
-    for (int j = 0; j < D / 32; ++j)
+    for (int j = 0; j < kColumns / 8; ++j)
         out[j] = make_uint4(Pair<T>::join(o[8 * j] * inv, o[8 * j + 1] * inv), Pair<T>::join(o[8 * j + 2] * inv, o[8 * j + 3] * inv),
                             Pair<T>::join(o[8 * j + 4] * inv, o[8 * j + 5] * inv), Pair<T>::join(o[8 * j + 6] * inv, o[8 * j + 7] * inv));
-    if (wid == 0 && P.lse) P.lse[row * P.n_q_heads + h] = l > 0.f ? (m + log2f(l)) * 0x1.62e43p-1f : -INFINITY;
+    if (column == 0 && P.lse) P.lse[row * P.n_q_heads + h] = l > 0.f ? (m + log2f(l)) * 0x1.62e43p-1f : -INFINITY;
 }
 
 using EncodeTiled = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*,
@@ -244,8 +265,9 @@ cudaError_t launch_merge(const AttentionParams& p, int blocks, int rows, bool co
                       : (wide ? merge_kernel<__half, 128> : merge_kernel<__half, 64>);
     auto by_columns = bf ? (wide ? merge_columns_kernel<__nv_bfloat16, 128> : merge_columns_kernel<__nv_bfloat16, 64>)
                          : (wide ? merge_columns_kernel<__half, 128> : merge_columns_kernel<__half, 64>);
-    return launch_dependent(columns ? by_columns : by_rows, dim3((unsigned)blocks, (unsigned)(y > few ? y : few)), dim3(kThreads), 0, 1, stream,
-                            p, blocks, rows);
+    const unsigned z = columns ? p.cache.head_dim / (kColumns * (kThreads / 32)) : 1;
+    return launch_dependent(columns ? by_columns : by_rows, dim3((unsigned)blocks, (unsigned)(y > few ? y : few), z), dim3(kThreads), 0, 1,
+                            stream, p, blocks, rows);
 }
 
 size_t attention_workspace(const ctr_kv_cache& cache, int32_t n_q_heads, int32_t, int32_t max_nodes)
