@@ -35,7 +35,8 @@ struct Layout {
     // the softmax takes over: at launch 384 x 168, then 256 x 216 + 128 x 72, the same sum
     static constexpr int kThreads = kTiles == 1 ? 192 : 384;
     static constexpr int kBlocksPerSm = kTiles == 1 ? 2 : 1;
-    static constexpr int kItemCost = kTiles == 1 ? 4 : 6;      // measured: 12,000 cycles, of 2,900 and 1,900 a unit
+    // units; 32 trees of 16: 44.0 us at 4, 43.0 at 7, 43.8 at 10; two tiles, wide trees: 216.8 at 6, 215.3 at 12, 217.6 at 18
+    static constexpr int kItemCost = kTiles == 1 ? 7 : 10;
     static constexpr int kSlot = kKeys * D * 2;                // bytes of a ring slot: a unit's keys or its values
     static constexpr int kQ = kRows * D * 2;
     static constexpr int kSlots = kTiles == 1 ? 5 : 10;
