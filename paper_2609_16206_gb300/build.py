@@ -10,14 +10,20 @@ build(checked=True) compiles the same sources with CTR_BOUNDS_CHECK=1 into
 _build_checked/ and libctr_checked.so: the simulator then checks every index
 into its workspace, the trace and the outputs (see ctr_bounds_checked in
 include/ctr.h).  build_all() makes both libraries from one pool of jobs.
+
+Either also makes _marshal.so, the Python module that reads the tensors of the
+decode operators' calls (csrc/marshal.cpp, by the host compiler, against the
+installed torch).
 """
 from __future__ import annotations
 
 import concurrent.futures as cf
+import importlib.util
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -33,6 +39,7 @@ DECODE_SOURCES = ["decode_api.cu", "kv_append.cu", "tree_attention.cu", "attenti
                   "sample.cu"]
 DECODE_HEADERS = [os.path.join(CSRC, "decode_internal.cuh"), os.path.join(CSRC, "attention_internal.cuh"), os.path.join(ROOT, "include", "ctr_decode.h"),
                   os.path.join(ROOT, "include", "ctr.h")]
+MARSHAL = os.path.join(HERE, "_marshal.so")
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 COMMON = ["-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall",
           "-I", os.path.join(ROOT, "include")]
@@ -77,6 +84,28 @@ def _jobs(checked: bool, force: bool, ptxas_info: bool):
     return jobs, objs, lib
 
 
+def _marshal_job(force: bool):
+    """The command that makes _marshal.so, if it is due; its output goes beside it first, and _run moves it."""
+    src = os.path.join(CSRC, "marshal.cpp")
+    torch = os.path.dirname(importlib.util.find_spec("torch").origin)
+    deps = [src, os.path.join(ROOT, "include", "ctr_decode.h"), os.path.join(ROOT, "include", "ctr.h"),
+            os.path.join(torch, "version.py")]
+    if not force and not _stale(MARSHAL, deps):
+        return []
+    cxx = shutil.which("g++") or shutil.which("c++")
+    if not cxx:
+        raise RuntimeError("no host C++ compiler found; it is required to build _marshal.so")
+    lib = os.path.join(torch, "lib")
+    return [[cxx, "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-Wall",
+             "-isystem", sysconfig.get_paths()["include"], "-isystem", os.path.join(torch, "include"),
+             "-isystem", os.path.join(torch, "include", "torch", "csrc", "api", "include"), src, "-o", _beside(MARSHAL),
+             "-L" + lib, "-ltorch_python", "-ltorch_cpu", "-lc10"]]
+
+
+def _beside(target: str) -> str:
+    return target + f".tmp{os.getpid()}"
+
+
 def _run(jobs, verbose: bool, ptxas_info: bool):
     if not jobs:
         return
@@ -86,12 +115,14 @@ def _run(jobs, verbose: bool, ptxas_info: bool):
         if verbose or ptxas_info or r.returncode != 0:
             sys.stderr.write(r.stdout + r.stderr)
         if r.returncode != 0:
-            raise RuntimeError("nvcc failed: " + " ".join(cmd))
+            raise RuntimeError("compiler failed: " + " ".join(cmd))
+    if os.path.exists(_beside(MARSHAL)):
+        os.replace(_beside(MARSHAL), MARSHAL)
 
 
 def _link(objs, lib, relink: bool):
     if relink or _stale(lib, objs):
-        tmp = lib + f".tmp{os.getpid()}"
+        tmp = _beside(lib)
         r = subprocess.run([nvcc()] + ARCH + ["-shared", "-o", tmp] + objs, capture_output=True, text=True)
         if r.returncode != 0:
             sys.stderr.write(r.stdout + r.stderr)
@@ -101,7 +132,7 @@ def _link(objs, lib, relink: bool):
 
 def build(force: bool = False, verbose: bool = False, ptxas_info: bool = False, checked: bool = False) -> str:
     jobs, objs, lib = _jobs(checked, force, ptxas_info)
-    _run(jobs, verbose, ptxas_info)
+    _run(jobs + _marshal_job(force), verbose, ptxas_info)
     _link(objs, lib, force or bool(jobs))
     return lib
 
@@ -110,7 +141,7 @@ def build_all(force: bool = False, verbose: bool = False) -> tuple:
     """libctr.so and libctr_checked.so, their translation units compiled in one pool."""
     plain = _jobs(False, force, False)
     checked = _jobs(True, force, False)
-    _run(plain[0] + [job for job in checked[0] if job not in plain[0]], verbose, False)
+    _run(plain[0] + [job for job in checked[0] if job not in plain[0]] + _marshal_job(force), verbose, False)
     _link(plain[1], plain[2], force or bool(plain[0]))
     _link(checked[1], checked[2], force or bool(checked[0]))
     return plain[2], checked[2]

@@ -1,0 +1,203 @@
+// marshal.cpp -- reads the tensors of a call of the decode operators (include/ctr_decode.h) and makes the call.
+//
+// The Python module _marshal: what ctr.py's wrappers would do with each tensor's attributes (type, shape, strides,
+// device, pointer: about 70 ns each from Python, and 1.3 us for a call of 20 arguments through ctypes) in one call of
+// its own.  A small append takes 3 us of the host in place of 8, of which the launch is 1.8.  A tensor that does not
+// fit raises ValueError; what the entry point returns is the result.
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <exception>
+
+#include "../../include/ctr_decode.h"
+
+namespace {
+
+decltype(&ctr_kv_append) append_entry = nullptr;
+decltype(&ctr_tree_attention) attention_entry = nullptr;
+decltype(&ctr_sample) sample_entry = nullptr;
+
+struct Refused {};  // the Python error is set
+
+template <typename... Args>
+[[noreturn]] void refuse(const char* format, Args... args)
+{
+    PyErr_Format(PyExc_ValueError, format, args...);
+    throw Refused{};
+}
+
+const char* name_of(at::ScalarType type)
+{
+    switch (type) {
+        case at::kBFloat16: return "torch.bfloat16";
+        case at::kHalf: return "torch.float16";
+        case at::kFloat: return "torch.float32";
+        case at::kInt: return "torch.int32";
+        case at::kLong: return "torch.int64";
+        default: return "another type";
+    }
+}
+int code_of(at::ScalarType type) { return type == at::kBFloat16 ? CTR_BF16 : type == at::kHalf ? CTR_F16 : type == at::kFloat ? CTR_F32 : -1; }
+
+const at::Tensor& tensor(PyObject* o, const char* name)
+{
+    if (!THPVariable_Check(o)) refuse("%s must be a tensor", name);
+    return THPVariable_Unpack(o);
+}
+
+long long integer(PyObject* o)
+{
+    const long long v = PyLong_AsLongLong(o);
+    if (v == -1 && PyErr_Occurred()) throw Refused{};
+    return v;
+}
+void* address(PyObject* o) { return reinterpret_cast<void*>(static_cast<uintptr_t>(integer(o))); }
+// sizes past 32 bits are refused by the entry points like the largest that is not
+int32_t narrow(int64_t v) { return (int32_t)std::min<int64_t>(std::max<int64_t>(v, INT32_MIN), INT32_MAX); }
+
+// [tokens, heads, head_dim] in the cache's type, the last dimension contiguous
+ctr_rows rows_of(const at::Tensor& t, const ctr_kv_cache& cache, const char* name)
+{
+    const at::ScalarType type = cache.dtype == CTR_BF16 ? at::kBFloat16 : at::kHalf;
+    if (t.dim() != 3 || t.scalar_type() != type || t.size(2) != cache.head_dim || !t.is_cuda() || (t.stride(2) != 1 && t.numel() > 0))
+        refuse("%s must be a CUDA tensor [tokens, heads, %d] of %s, the last dimension contiguous", name, (int)cache.head_dim, name_of(type));
+    return ctr_rows{t.data_ptr(), t.stride(0), t.stride(1)};
+}
+
+// a contiguous tensor of n elements; None gives a null pointer
+template <typename T>
+T* vector_of(PyObject* o, at::ScalarType type, int64_t n, const char* name)
+{
+    if (o == Py_None) return nullptr;
+    const at::Tensor& t = tensor(o, name);
+    if (t.scalar_type() != type || t.numel() != n || !t.is_cuda() || !t.is_contiguous())
+        refuse("%s must be a contiguous CUDA tensor of %lld elements of %s", name, (long long)n, name_of(type));
+    return static_cast<T*>(t.data_ptr());
+}
+
+// The body of a method: its count of arguments checked, no C++ exception past it.
+template <typename Body>
+PyObject* method(Py_ssize_t n, Py_ssize_t expected, Body&& body)
+{
+    if (n != expected) {
+        PyErr_Format(PyExc_TypeError, "expected %zd arguments, got %zd", expected, n);
+        return nullptr;
+    }
+    try {
+        return PyLong_FromLong(body());
+    } catch (const Refused&) {
+    } catch (const std::exception& e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "unknown error");
+    }
+    return nullptr;
+}
+// The call itself, other Python threads running: a launch can wait for room in the stream's queue.
+template <typename Call>
+int released(Call&& call)
+{
+    int rc;
+    Py_BEGIN_ALLOW_THREADS
+    rc = call();
+    Py_END_ALLOW_THREADS
+    return rc;
+}
+
+// bind(ctr_kv_append, ctr_tree_attention, ctr_sample): the addresses of the loaded library's entry points
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return method(n, 3, [&] {
+        append_entry = reinterpret_cast<decltype(append_entry)>(address(a[0]));
+        attention_entry = reinterpret_cast<decltype(attention_entry)>(address(a[1]));
+        sample_entry = reinterpret_cast<decltype(sample_entry)>(address(a[2]));
+        return 0;
+    });
+}
+
+// kv_append(cache, rope, q, k, v, positions, slots, q_out, stream); cache, rope, stream: addresses
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return method(n, 9, [&] {
+        const auto* cache = static_cast<const ctr_kv_cache*>(address(a[0]));
+        const auto* rope = static_cast<const ctr_rope*>(address(a[1]));
+        const at::Tensor &q = tensor(a[2], "q"), &k = tensor(a[3], "k"), &v = tensor(a[4], "v"), &q_out = tensor(a[7], "q_out");
+        if (k.dim() != 3 || k.sizes() != v.sizes() || k.size(1) != cache->n_kv_heads || q.sizes() != q_out.sizes() || q.dim() != 3 ||
+            q.size(0) != k.size(0))
+            refuse("q, k, v and q_out must be [tokens, heads, head_dim] with the cache's heads");
+        const ctr_rows rq = rows_of(q, *cache, "q"), rk = rows_of(k, *cache, "k"), rv = rows_of(v, *cache, "v"), ro = rows_of(q_out, *cache, "q_out");
+        const int64_t tokens = k.size(0);
+        const auto* positions = vector_of<const int64_t>(a[5], at::kLong, tokens, "positions");
+        const auto* slots = vector_of<const int64_t>(a[6], at::kLong, tokens, "slots");
+        const int32_t heads = narrow(q.size(1));
+        void* stream = address(a[8]);
+        return released([&] { return append_entry(cache, rope, rq, rk, rv, ro, tokens, heads, positions, slots, stream); });
+    });
+}
+
+// tree_attention(cache, q, q_start, kv_len, page_table, out, workspace, max_nodes, tree_mask, lse, scale, status, stream)
+PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return method(n, 13, [&] {
+        const auto* cache = static_cast<const ctr_kv_cache*>(address(a[0]));
+        const at::Tensor &q = tensor(a[1], "q"), &lens = tensor(a[3], "kv_len"), &table = tensor(a[4], "page_table"), &out = tensor(a[5], "out"),
+                         &workspace = tensor(a[6], "workspace");
+        const int64_t seqs = lens.numel();
+        if (out.sizes() != q.sizes() || table.dim() != 2 || table.size(0) != seqs)
+            refuse("out must have q's shape, page_table must be int32 [n_seqs, width]");
+        const ctr_rows rq = rows_of(q, *cache, "q"), ro = rows_of(out, *cache, "out");
+        const int64_t rows = q.size(0), heads = q.size(1);
+        const auto* start = vector_of<const int32_t>(a[2], at::kInt, seqs + 1, "q_start");
+        const auto* kv_len = vector_of<const int32_t>(a[3], at::kInt, seqs, "kv_len");
+        const auto* pages = vector_of<const int32_t>(a[4], at::kInt, seqs * table.size(1), "page_table");
+        if (!workspace.is_cuda() || !workspace.is_contiguous()) refuse("workspace must be a contiguous CUDA tensor");
+        const int32_t nodes = narrow(integer(a[7]));
+        const auto* mask = reinterpret_cast<const uint64_t*>(vector_of<const int64_t>(a[8], at::kLong, rows, "tree_mask"));
+        auto* lse = vector_of<float>(a[9], at::kFloat, rows * heads, "lse");
+        const double scale = PyFloat_AsDouble(a[10]);
+        if (scale == -1.0 && PyErr_Occurred()) throw Refused{};
+        auto* status = vector_of<int32_t>(a[11], at::kInt, 1, "status");
+        void* stream = address(a[12]);
+        return released([&] {
+            return attention_entry(cache, rq, ro, rows, narrow(heads), narrow(seqs), nodes, start, kv_len, pages, narrow(table.size(1)), mask,
+                                   (float)scale, lse, status, workspace.data_ptr(), workspace.nbytes(), stream);
+        });
+    });
+}
+
+// sample(logits, temperature, u, token, top_k, top_p, min_p, logprob, n_kept, stream)
+PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n)
+{
+    return method(n, 10, [&] {
+        const at::Tensor& x = tensor(a[0], "logits");
+        const int dtype = code_of(x.scalar_type());
+        if (x.dim() != 2 || dtype < 0 || !x.is_cuda() || (x.stride(1) != 1 && x.size(1) > 1))
+            refuse("logits must be a CUDA tensor [rows, vocab] of a floating type, the last dimension contiguous");
+        const int64_t rows = x.size(0), vocab = x.size(1);
+        const auto* temperature = vector_of<const float>(a[1], at::kFloat, rows, "temperature");
+        const auto* u = vector_of<const float>(a[2], at::kFloat, rows, "u");
+        auto* token = vector_of<int32_t>(a[3], at::kInt, rows, "token");
+        const auto* top_k = vector_of<const int32_t>(a[4], at::kInt, rows, "top_k");
+        const auto* top_p = vector_of<const float>(a[5], at::kFloat, rows, "top_p");
+        const auto* min_p = vector_of<const float>(a[6], at::kFloat, rows, "min_p");
+        auto* logprob = vector_of<float>(a[7], at::kFloat, rows, "logprob");
+        auto* n_kept = vector_of<int32_t>(a[8], at::kInt, rows, "n_kept");
+        void* stream = address(a[9]);
+        return released([&] {
+            return sample_entry(x.data_ptr(), dtype, rows > 1 ? x.stride(0) : vocab, rows, narrow(vocab), temperature, top_k, top_p, min_p, u, token,
+                                logprob, n_kept, stream);
+        });
+    });
+}
+
+PyMethodDef methods[] = {{"bind", (PyCFunction)(void (*)())bind, METH_FASTCALL, nullptr},
+                         {"kv_append", (PyCFunction)(void (*)())kv_append, METH_FASTCALL, nullptr},
+                         {"tree_attention", (PyCFunction)(void (*)())tree_attention, METH_FASTCALL, nullptr},
+                         {"sample", (PyCFunction)(void (*)())sample, METH_FASTCALL, nullptr},
+                         {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module_def = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__marshal(void) { return PyModule_Create(&module_def); }

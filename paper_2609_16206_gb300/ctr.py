@@ -1,14 +1,17 @@
-"""ctypes binding of libctr.so (include/ctr.h, include/ctr_decode.h).
+"""Binding of libctr.so: include/ctr.h by ctypes, the calls of
+include/ctr_decode.h by the extension module ``_marshal`` (csrc/marshal.cpp).
 
 Argument marshalling only: configurations (the dataclasses of ``workloads``)
 become the C structs of ``ctr.h``; torch tensors become device pointers; the
 current torch stream is passed as ``cudaStream_t``.  Every step of the
 computation runs in the CUDA kernels of ``csrc/``.  There is no fallback: if
-``libctr.so`` is missing or CUDA is unavailable the calls raise.
+``libctr.so`` or the module is missing or CUDA is unavailable the calls raise.
 """
 from __future__ import annotations
 
 import ctypes as C
+import importlib.machinery
+import importlib.util
 import os
 import threading
 
@@ -17,6 +20,7 @@ import torch
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libctr.so")
+MARSHAL_PATH = os.path.join(_HERE, "_marshal.so")
 # the bounds-checked build of the same library (build.build(checked=True)); use_library() switches to it
 LIB_CHECKED_PATH = os.path.join(_HERE, "libctr_checked.so")
 
@@ -143,14 +147,34 @@ def lib():
     return _lib
 
 
+_marshal = None
+
+
+def marshal():
+    """The module that makes the decode operators' calls, bound to the loaded library."""
+    global _marshal
+    with _lock:
+        if _marshal is None:
+            if not os.path.exists(MARSHAL_PATH):
+                msg = f"{MARSHAL_PATH} is missing: build it with paper_2609_16206_gb300/build.py"
+                raise CtrError("load", CTR_ECUDA, detail=msg) from FileNotFoundError(msg)
+            loader = importlib.machinery.ExtensionFileLoader("_marshal", MARSHAL_PATH)
+            m = importlib.util.module_from_spec(importlib.util.spec_from_loader("_marshal", loader))
+            loader.exec_module(m)
+            L = lib()
+            m.bind(*(C.cast(f, C.c_void_p).value for f in (L.ctr_kv_append, L.ctr_tree_attention, L.ctr_sample)))
+            _marshal = m
+    return _marshal
+
+
 def use_library(path: str) -> str:
     """Make every following call go to the library at `path` (LIB_PATH or
     LIB_CHECKED_PATH); returns the path in use before."""
-    global _lib, LIB_PATH
+    global _lib, _marshal, LIB_PATH
     with _lock:
         before = LIB_PATH
         LIB_PATH = path
-        _lib = None
+        _lib = _marshal = None
         lib()
     return before
 
@@ -357,7 +381,7 @@ class KvCache:
         self.n_pages, self.n_kv_heads, self.page_tokens, self.head_dim = k.shape
         self.struct = CtrKvCache(k.data_ptr(), v.data_ptr(), _DTYPES[k.dtype], self.n_kv_heads, self.head_dim,
                                  self.page_tokens, self.n_pages, k.stride(0), k.stride(1), k.stride(2))
-        self.ref = C.byref(self.struct)
+        self.address = C.addressof(self.struct)
 
 
 class Rope:
@@ -370,52 +394,30 @@ class Rope:
         self.turns = turns
         self.rot_dim = 2 * turns.numel()
         self.struct = CtrRope(_ptr(turns), self.rot_dim, int(bool(interleaved)), float(scale), 0)
-        self.ref = C.byref(self.struct)
-
-
-def _rows(t, cache, name):
-    """[tokens, heads, head_dim] in the cache's dtype, the last dimension contiguous."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or t.dtype is not cache.dtype or shape[2] != cache.head_dim or not t.is_cuda or \
-            (stride[2] != 1 and t.numel() > 0):
-        raise ValueError(f"{name} must be a CUDA tensor [tokens, heads, {cache.head_dim}] of {cache.dtype}, the last "
-                         "dimension contiguous")
-    return CtrRows(t.data_ptr(), stride[0], stride[1])
-
-
-def _vector(t, dtype, n, name):
-    if t is None:
-        return None
-    if t.dtype is not dtype or t.numel() != n or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name} must be a contiguous CUDA tensor of {n} elements of {dtype}")
-    return t.data_ptr()
+        self.address = C.addressof(self.struct)
 
 
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)  # absent without CUDA
 
 
 def _stream_on(stream, index):
-    """The given stream's handle, or the current one's of device `index`."""
-    return _raw_stream(index) if stream is None else stream.cuda_stream
+    """The given stream's handle, or the current one's of device `index` (None: the tensor is on the host, and refused)."""
+    if stream is not None:
+        return stream.cuda_stream
+    return 0 if index is None else _raw_stream(index)
 
 
 def ctr_kv_append(cache: KvCache, rope: Rope, q, k, v, positions, slots, q_out, stream=None):
     """Rotate q into q_out, append the rotated k and v to their slots.  q, k, v: [tokens, heads, head_dim]; positions
     and slots: int64 per token (slot < 0: padding)."""
-    k_shape, q_shape = k.shape, q.shape
-    n = k_shape[0]
-    if k_shape != v.shape or len(k_shape) != 3 or k_shape[1] != cache.n_kv_heads or q_shape != q_out.shape or q_shape[0] != n:
-        raise ValueError("q, k, v and q_out must be [tokens, heads, head_dim] with the cache's heads")
-    rc = (_lib or lib()).ctr_kv_append(
-        cache.ref, rope.ref, _rows(q, cache, "q"), _rows(k, cache, "k"), _rows(v, cache, "v"),
-        _rows(q_out, cache, "q_out"), n, q_shape[1], _vector(positions, torch.int64, n, "positions"),
-        _vector(slots, torch.int64, n, "slots"), _stream_on(stream, cache.index))
+    rc = (_marshal or marshal()).kv_append(cache.address, rope.address, q, k, v, positions, slots, q_out,
+                                           _stream_on(stream, cache.index))
     if rc:
         raise CtrError("ctr_kv_append", rc)
 
 
 def attention_workspace(cache: KvCache, n_q_heads: int, n_seqs: int, max_nodes: int) -> torch.Tensor:
-    n = int(lib().ctr_attention_workspace_bytes(cache.ref, int(n_q_heads), int(n_seqs), int(max_nodes)))
+    n = int(lib().ctr_attention_workspace_bytes(C.byref(cache.struct), int(n_q_heads), int(n_seqs), int(max_nodes)))
     if n == 0:
         raise CtrError("ctr_attention_workspace_bytes", CTR_EINVAL)
     return torch.empty(n, dtype=torch.uint8, device=cache.device)
@@ -426,17 +428,9 @@ def ctr_tree_attention(cache: KvCache, q, q_start, kv_len, page_table, out, work
     """Attention of the new tokens (rows of q, sequence b's from q_start[b] to q_start[b + 1]) over the cache that holds
     them.  q, out: [rows, heads, head_dim]; q_start int32 [n_seqs + 1]; kv_len int32 [n_seqs]; page_table int32
     [n_seqs, width]; tree_mask int64 [rows] (bit j: attends to new token j; None: a chain); lse fp32 [rows, heads]."""
-    q_shape, table_shape = q.shape, page_table.shape
-    rows, heads, n_seqs = q_shape[0], q_shape[1], kv_len.numel()
-    if out.shape != q_shape or len(table_shape) != 2 or table_shape[0] != n_seqs:
-        raise ValueError("out must have q's shape, page_table must be int32 [n_seqs, width]")
-    rc = (_lib or lib()).ctr_tree_attention(
-        cache.ref, _rows(q, cache, "q"), _rows(out, cache, "out"), rows, heads, n_seqs, max_nodes,
-        _vector(q_start, torch.int32, n_seqs + 1, "q_start"), _vector(kv_len, torch.int32, n_seqs, "kv_len"),
-        _vector(page_table, torch.int32, n_seqs * table_shape[1], "page_table"), table_shape[1],
-        _vector(tree_mask, torch.int64, rows, "tree_mask"), cache.head_dim ** -0.5 if scale is None else scale,
-        _vector(lse, torch.float32, rows * heads, "lse"), _vector(status, torch.int32, 1, "status"), _ptr(workspace),
-        workspace.nbytes, _stream_on(stream, cache.index))
+    rc = (_marshal or marshal()).tree_attention(
+        cache.address, q, q_start, kv_len, page_table, out, workspace, max_nodes, tree_mask, lse,
+        cache.head_dim ** -0.5 if scale is None else scale, status, _stream_on(stream, cache.index))
     if rc:
         raise CtrError("ctr_tree_attention", rc)
 
@@ -444,15 +438,7 @@ def ctr_tree_attention(cache: KvCache, q, q_start, kv_len, page_table, out, work
 def ctr_sample(logits, temperature, u, token, top_k=None, top_p=None, min_p=None, logprob=None, n_kept=None, stream=None):
     """A token per row of logits [rows, vocab] (bfloat16, float16 or float32, rows of any stride).  Per row: temperature,
     u in [0, 1), top_p and min_p fp32; top_k, token and n_kept int32; logprob fp32."""
-    shape, stride, dtype = logits.shape, logits.stride(), _DTYPES.get(logits.dtype)
-    if len(shape) != 2 or dtype is None or not logits.is_cuda or (stride[1] != 1 and shape[1] > 1):
-        raise ValueError("logits must be a CUDA tensor [rows, vocab] of a floating type, the last dimension contiguous")
-    n, vocab = shape
-    f32, i32 = torch.float32, torch.int32
-    rc = (_lib or lib()).ctr_sample(
-        logits.data_ptr(), dtype, stride[0] if n > 1 else vocab, n, vocab,
-        _vector(temperature, f32, n, "temperature"), _vector(top_k, i32, n, "top_k"), _vector(top_p, f32, n, "top_p"),
-        _vector(min_p, f32, n, "min_p"), _vector(u, f32, n, "u"), _vector(token, i32, n, "token"),
-        _vector(logprob, f32, n, "logprob"), _vector(n_kept, i32, n, "n_kept"), _stream_on(stream, logits.device.index))
+    rc = (_marshal or marshal()).sample(logits, temperature, u, token, top_k, top_p, min_p, logprob, n_kept,
+                                        _stream_on(stream, logits.device.index))
     if rc:
         raise CtrError("ctr_sample", rc)
