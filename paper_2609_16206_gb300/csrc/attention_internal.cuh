@@ -284,7 +284,7 @@ cudaError_t launch_merge(const AttentionParams& p, int blocks, int rows, bool co
 int sm_count();  // of the current device
 size_t stream_workspace(int rows, int d);
 size_t tiles_workspace(int rows, int d);
-cudaError_t launch_tiles(const AttentionParams& p, cudaStream_t stream);  // more than 32 rows a KV head
+cudaError_t launch_tiles(const AttentionParams& p, cudaStream_t stream);
 cudaError_t launch_stream(const AttentionParams& p, cudaStream_t stream);
 
 }  // namespace ctr

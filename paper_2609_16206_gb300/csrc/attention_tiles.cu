@@ -1,5 +1,5 @@
-// attention_tiles.cu -- tree attention where more than 32 query rows share a
-// KV head (see tree_attention.cu): both products on the tensor cores' tcgen05
+// attention_tiles.cu -- tree attention where more query rows share a KV head
+// than attention_stream.cu takes: both products on the tensor cores' tcgen05
 // path, 128 rows to a tile.
 //
 // S = Q K^T comes into tensor memory from shared memory; a warpgroup takes a
@@ -10,11 +10,19 @@
 // the sums changes no rounding that matters, and few tiles do).  One warp loads
 // keys and values by TMA into a ring, one thread issues the products.
 //
-// Up to 128 rows: the cache's bytes are the bound; 64 tokens a tile, two blocks
-// an SM, so that one block's begin and end of an item hide behind the other.
+// Up to 160 rows: the cache's bytes are the bound; two blocks an SM, so that one
+// block's begin and end of an item hide behind the other.  Measured (fp16, 32
+// trees of 16 nodes, 4 query heads to a KV head, 160 MB of cache in 43.0 us):
+// 3.7 TB/s; a block has some 17 units of 64 tokens, and its items' begin and end
+// cost it seven.
 // More: the tensor cores are; a block takes 256 rows as two tiles whose
-// softmaxes and products alternate, over 128 tokens at a time, which also
-// reads the cache half as often.
+// softmaxes and products run beside each other, which also reads the cache half
+// as often.  Measured (bf16, 16 trees of 64 nodes, 8 query heads to a KV head,
+// 8,192 tokens of context: 215 us): 0.98 PFLOP/s.  The products of 128 x 64
+// scores read both operands from shared memory and take it for half as long
+// again as their arithmetic.  Units of 128 tokens would not, but leave tensor
+// memory for one region of scores a tile only: 256 us, or 290 with two threads a
+// row; scores read twice in place of 64 registers of them: 235 us.
 #include <type_traits>
 
 #include "attention_internal.cuh"
@@ -584,10 +592,14 @@ cudaError_t launch(const AttentionParams& p, cudaStream_t stream)
     return launch_merge(p, blocks, L::kRows, true, stream);
 }
 
+// One tile a block up to so many rows of a KV head.  32 trees over 1,000 tokens each, 8 query heads to a KV head, one
+// tile and two: 160 rows 56.3 and 58.3 us, 192 rows 62.4 and 60.6, 512 rows 126 and 105.
+constexpr int kOneTileRows = 160;
+
 template <typename T>
 cudaError_t launch_typed(const AttentionParams& p, cudaStream_t stream)
 {
-    const bool two = p.group * p.max_nodes > 128;
+    const bool two = p.group * p.max_nodes > kOneTileRows;
     if (p.cache.head_dim == 64) return two ? launch<T, 64, 2>(p, stream) : launch<T, 64, 1>(p, stream);
     return two ? launch<T, 128, 2>(p, stream) : launch<T, 128, 1>(p, stream);
 }
@@ -596,7 +608,7 @@ cudaError_t launch_typed(const AttentionParams& p, cudaStream_t stream)
 
 size_t tiles_workspace(int rows, int d)
 {
-    const int tiles = rows > 128 ? 2 : 1, blocks = sm_count() * (tiles == 1 ? 2 : 1);
+    const int tiles = rows > kOneTileRows ? 2 : 1, blocks = sm_count() * (tiles == 1 ? 2 : 1);
     return slots_bytes(blocks) + (size_t)blocks * 2 * part_floats(128 * tiles, d) * sizeof(float);
 }
 
