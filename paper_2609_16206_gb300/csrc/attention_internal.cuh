@@ -113,6 +113,12 @@ struct __align__(16) SplitSlot {  // the item that a block begins and does not e
     int64_t reserved;
 };
 
+// a / b of two that are not negative, and mostly of 32 bits
+__device__ __forceinline__ int64_t divide(int64_t a, int64_t b)
+{
+    if (((uint64_t)(a | b) >> 32) == 0) return (uint32_t)a / (uint32_t)b;
+    return a / b;
+}
 __device__ __forceinline__ int units_of(const Seq& s, int unit)
 {
     return s.n_new == 0 ? 0 : s.len <= unit ? 1 : (s.len + unit - 1) / unit;
@@ -129,54 +135,86 @@ struct Range {
     int item_cost, blocks;      // blocks with work: each has a unit at least
     int b;                      // the sequence that it begins in, and where in it (over its items)
     int64_t within;
+    Seq s;
+
+    __device__ __forceinline__ void cut(int64_t units, int64_t items, int c, int grid, int cost)
+    {
+        item_cost = units < (int64_t)kFewUnits * grid ? 0 : cost;
+        total = units + item_cost * items;
+        blocks = (int)min((int64_t)grid, divide(total, 1 + item_cost));
+        begin = end = within = 0;
+        b = 0;
+        if (c >= blocks) return;
+        begin = divide(total * c, blocks);
+        end = divide(total * (c + 1), blocks);
+    }
 };
 
-// The range of block c; by all threads of the block.  scratch: 2 * kThreads / 32 + 2 words of 64 bits.
+// The range of block c; by all threads of the block.  scratch: 2 * kThreads / 32 + 2 words of 64 bits.  (A block's begin
+// and end run once, from a cold instruction cache: short code counts there, and each warp for itself where it can.)
 template <int kThreads>
 __device__ Range find_range(const AttentionParams& P, int unit, int item_rows, int item_cost, int c, int blocks, int64_t* scratch)
 {
     constexpr int kWarps = kThreads / 32;
     const int tid = threadIdx.x, lane = tid & 31, wid = tid >> 5;
-    const int per = (P.n_seqs + kThreads - 1) / kThreads;
-    const int first = min(tid * per, P.n_seqs), last = min(first + per, P.n_seqs);
-    int64_t my_items = 0, my_units = 0;
+    const bool few = P.n_seqs <= 32;  // a lane a sequence, in every warp
+    const int per = few ? 1 : (P.n_seqs + kThreads - 1) / kThreads;
+    const int first = few ? min(lane, P.n_seqs) : min(tid * per, P.n_seqs), last = min(first + per, P.n_seqs);
+    int my_items = 0;
+    int64_t my_units = 0;
+    Seq s = {0, 0, 0, 0};
+#pragma unroll 1
     for (int b = first; b < last; ++b) {
-        const Seq s = seq_of(P, b);
+        s = seq_of(P, b);
         const int units = units_of(s, unit), items = units > 0 ? P.cache.n_kv_heads * groups_of(P, s, item_rows) : 0;
         my_items += items;
         my_units += (int64_t)items * units;
     }
-    int64_t items = my_items, units = my_units;  // of the threads up to this one
-#pragma unroll
+    int items = my_items;  // of the threads up to this one
+    int64_t units = my_units;
+#pragma unroll 1
     for (int off = 1; off < 32; off <<= 1) {
-        const int64_t i = __shfl_up_sync(~0u, items, off), u = __shfl_up_sync(~0u, units, off);
+        const int i = __shfl_up_sync(~0u, items, off);
+        const int64_t u = __shfl_up_sync(~0u, units, off);
         if (lane >= off) items += i, units += u;
     }
-    if (lane == 31) {
-        scratch[2 * wid] = items;
-        scratch[2 * wid + 1] = units;
-    }
-    __syncthreads();
-    int64_t all_items = 0, all_units = 0;
-#pragma unroll
-    for (int w = 0; w < kWarps; ++w) {
-        if (w == wid) items += all_items, units += all_units;
-        all_items += scratch[2 * w];
-        all_units += scratch[2 * w + 1];
+    int all_items = __shfl_sync(~0u, items, 31);
+    int64_t all_units = __shfl_sync(~0u, units, 31);
+    if (!few) {
+        if (lane == 31) {
+            scratch[2 * wid] = items;
+            scratch[2 * wid + 1] = units;
+        }
+        __syncthreads();
+        all_items = 0;
+        all_units = 0;
+#pragma unroll 1
+        for (int w = 0; w < kWarps; ++w) {
+            if (w == wid) items += all_items, units += all_units;
+            all_items += (int)scratch[2 * w];
+            all_units += scratch[2 * w + 1];
+        }
     }
     Range r;
-    r.item_cost = all_units < (int64_t)kFewUnits * blocks ? 0 : item_cost;
-    r.total = all_units + r.item_cost * all_items;
-    r.blocks = (int)min((int64_t)blocks, r.total / (1 + r.item_cost));
-    r.begin = r.end = r.within = 0;
-    r.b = 0;
+    r.cut(all_units, all_items, c, blocks, item_cost);
+    r.s = s;
     if (c >= r.blocks) return r;  // the whole block
-    r.begin = r.total * c / r.blocks;
-    r.end = r.total * (c + 1) / r.blocks;
-    int64_t at = units - my_units + r.item_cost * (items - my_items);
-    if (at <= r.begin && r.begin < units + r.item_cost * items) {
+    int64_t at = units - my_units + (int64_t)r.item_cost * (items - my_items);
+    const bool here = at <= r.begin && r.begin < units + (int64_t)r.item_cost * items;
+    if (few) {
+        const int of = __ffs(__ballot_sync(~0u, here)) - 1;
+        r.b = of;
+        r.within = r.begin - __shfl_sync(~0u, at, of);
+        r.s.row0 = __shfl_sync(~0u, s.row0, of);
+        r.s.n_new = __shfl_sync(~0u, s.n_new, of);
+        r.s.len = __shfl_sync(~0u, s.len, of);
+        r.s.context = __shfl_sync(~0u, s.context, of);
+        return r;
+    }
+    if (here) {
+#pragma unroll 1
         for (int b = first; b < last; ++b) {
-            const Seq s = seq_of(P, b);
+            s = seq_of(P, b);
             const int u = units_of(s, unit);
             const int64_t n = u == 0 ? 0 : (int64_t)(u + r.item_cost) * P.cache.n_kv_heads * groups_of(P, s, item_rows);
             if (r.begin < at + n) {
@@ -190,6 +228,7 @@ __device__ Range find_range(const AttentionParams& P, int unit, int item_rows, i
     __syncthreads();
     r.b = (int)scratch[2 * kWarps];
     r.within = scratch[2 * kWarps + 1];
+    r.s = seq_of(P, r.b);
     return r;
 }
 
@@ -223,12 +262,12 @@ struct Walk {
         item_cost = r.item_cost;
         end = 0;
         if (left <= 0) return;
-        s = seq_of(P, b);
+        s = r.s;
         units = units_of(s, unit);
         groups = groups_of(P, s, item_rows);
-        const int64_t item = r.within / (units + item_cost), off = r.within - item * (units + item_cost);
-        head = (int)(item / groups);
-        group = (int)(item - (int64_t)head * groups);
+        const int64_t item = divide(r.within, units + item_cost), off = r.within - item * (units + item_cost);
+        head = (int)item / groups;  // fewer items than 2^31: n_kv_heads * groups
+        group = (int)item - head * groups;
         left += off;
         enter(off);
         load_ahead(P);
@@ -257,7 +296,7 @@ struct Walk {
     {
         SplitSlot d;
         const int64_t pos = r.end - left + item_cost + units - 1;
-        d.last = (int)(((pos + 1) * r.blocks - 1) / r.total);  // the largest c with floor(total c / blocks) <= pos
+        d.last = (int)divide((pos + 1) * r.blocks - 1, r.total);  // the largest c with floor(total c / blocks) <= pos
         d.rows = s.n_new * P.group - row0;
         d.row0 = row0;
         d.h = head;

@@ -236,17 +236,26 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
         // The warp's 32 queries, a row to D / 8 neighbouring lanes, copied from the item before's last scores on (from its
         // end, where its outputs go through their place).
         constexpr int kLanes = D / 8, kAtOnce = 32 / kLanes, kLoads = 32 / kAtOnce;
-        auto row_of = [&](const Walk& at, int i) { return at.group * L::kRows + 32 * wid + i * kAtOnce + lane / kLanes; };
         auto place_of = [&](int i) { return base + tile * 128 * D * 2 + piece(128, 32 * (wid & 3) + i * kAtOnce + lane / kLanes, lane % kLanes); };
-        auto copy_queries = [&](const Walk& at) {
+        // f(i, whether there is such a row, where its 16 bytes of this lane start in `rows`) for kLoads turns; each lane
+        // works one row's address out
+        auto each_row = [&](const Walk& at, const ctr_rows& rows, auto&& f) {
+            const int q = at.group * L::kRows + 32 * wid + lane, n = node_of(P, q);
+            const int64_t mine = (at.s.row0 + n) * rows.token_stride + (int64_t)(at.head * P.group + q - n * P.group) * rows.head_stride;
+            const uint32_t there = __ballot_sync(~0u, q < at.s.n_new * P.group);
 #pragma unroll 4
             for (int i = 0; i < kLoads; ++i) {
-                const int q = row_of(at, i), n = node_of(P, q);
-                const bool there = q < at.s.n_new * P.group && P.scale_log2 != 0.f;
-                const T* src = static_cast<const T*>(P.q.ptr);
-                if (there) src += (at.s.row0 + n) * P.q.token_stride + (int64_t)(at.head * P.group + q - n * P.group) * P.q.head_stride + 8 * (lane % kLanes);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(place_of(i)), "l"(src), "r"(there ? 16 : 0) : "memory");
+                const int of = i * kAtOnce + lane / kLanes;
+                const int64_t from = __shfl_sync(~0u, mine, of);
+                f(i, there >> of & 1, static_cast<T*>(rows.ptr) + from + 8 * (lane % kLanes));
             }
+        };
+        auto copy_queries = [&](const Walk& at) {
+            each_row(at, P.q, [&](int i, bool is, const T* src) {
+                const bool there = is && P.scale_log2 != 0.f;
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(place_of(i)), "l"(there ? src : static_cast<const T*>(P.q.ptr)), "r"(there ? 16 : 0)
+                             : "memory");
+            });
         };
         Walk ahead = w;
         if (w.more()) copy_queries(w);
@@ -428,15 +437,9 @@ tiles_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ 
             }
             if (whole) {  // the warp's rows, whole ones at a time
                 __syncwarp();
-                const int c = lane % kLanes;
-#pragma unroll 4
-                for (int i = 0; i < kLoads; ++i) {
-                    const int q = row_of(w, i), n = node_of(P, q);
-                    if (q < w.s.n_new * P.group)
-                        reinterpret_cast<uint4*>(static_cast<T*>(P.out.ptr) + (w.s.row0 + n) * P.out.token_stride +
-                                                 (int64_t)(head * P.group + q - n * P.group) * P.out.head_stride)[c] =
-                            *reinterpret_cast<const uint4*>(stage + piece(128, 32 * (wid & 3) + i * kAtOnce + lane / kLanes, c));
-                }
+                each_row(w, P.out, [&](int i, bool is, T* to) {
+                    if (is) *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(smem + (place_of(i) - base));
+                });
                 __syncwarp();
                 if (ahead.more()) copy_queries(ahead);
             }
