@@ -110,7 +110,6 @@ struct __align__(16) SplitSlot {  // the item that a block begins and does not e
     int32_t rows;              // of the item from row0 on (0: no such item)
     int32_t row0, h, last;     // first row of the sequence's KV head, the head, the block that ends the item
     int64_t first;             // the sequence's first row of q
-    int64_t reserved;
 };
 
 // a / b of two that are not negative, and mostly of 32 bits
@@ -301,7 +300,6 @@ struct Walk {
         d.row0 = row0;
         d.h = head;
         d.first = s.row0;
-        d.reserved = 0;
         return d;
     }
 };

@@ -109,12 +109,6 @@ __device__ __forceinline__ uint64_t add2(uint64_t a, uint64_t b)
     asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
     return r;
 }
-__device__ __forceinline__ uint64_t mul2(uint64_t a, uint64_t b)
-{
-    uint64_t r;
-    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
 __device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c)
 {
     uint64_t r;
@@ -174,7 +168,7 @@ struct SampleParams {
     int32_t* token;
     float* logprob;
     int32_t* n_kept;
-    uint64_t minus_zeros;       // two fp32 -0 (see mul2 in sample.cu)
+    uint64_t minus_zeros;       // two fp32 -0 (see Scale in sample.cu)
 };
 cudaError_t launch_sample(const SampleParams& p, cudaStream_t stream);
 
