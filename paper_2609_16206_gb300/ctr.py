@@ -129,16 +129,17 @@ def lib():
             L.ctr_simulate_noalloc.restype = C.c_int
             L.ctr_goodput.argtypes = [C.POINTER(CtrSimCfg), CtrRequests, i32, i32, i64, vp, vp, vp, vp, vp, vp]
             L.ctr_goodput.restype = C.c_int
-            L.ctr_kv_append.argtypes = [C.POINTER(CtrKvCache), C.POINTER(CtrRope), CtrRows, CtrRows, CtrRows, CtrRows,
-                                        i64, i32, vp, vp, vp]
-            L.ctr_kv_append.restype = C.c_int
-            L.ctr_attention_workspace_bytes.argtypes = [C.POINTER(CtrKvCache), i32, i32, i32]
-            L.ctr_attention_workspace_bytes.restype = C.c_size_t
-            L.ctr_tree_attention.argtypes = [C.POINTER(CtrKvCache), CtrRows, CtrRows, i64, i32, i32, i32, vp, vp, vp,
-                                             i32, vp, C.c_float, vp, vp, vp, C.c_size_t, vp]
-            L.ctr_tree_attention.restype = C.c_int
-            L.ctr_sample.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
-            L.ctr_sample.restype = C.c_int
+            if hasattr(L, "ctr_kv_append"):  # a build of the simulator's units alone has none of the decode operators
+                L.ctr_kv_append.argtypes = [C.POINTER(CtrKvCache), C.POINTER(CtrRope), CtrRows, CtrRows, CtrRows, CtrRows,
+                                            i64, i32, vp, vp, vp]
+                L.ctr_kv_append.restype = C.c_int
+                L.ctr_attention_workspace_bytes.argtypes = [C.POINTER(CtrKvCache), i32, i32, i32]
+                L.ctr_attention_workspace_bytes.restype = C.c_size_t
+                L.ctr_tree_attention.argtypes = [C.POINTER(CtrKvCache), CtrRows, CtrRows, i64, i32, i32, i32, vp, vp, vp,
+                                                 i32, vp, C.c_float, vp, vp, vp, C.c_size_t, vp]
+                L.ctr_tree_attention.restype = C.c_int
+                L.ctr_sample.argtypes = [vp, i32, i64, i64, i32, vp, vp, vp, vp, vp, vp, vp, vp, vp]
+                L.ctr_sample.restype = C.c_int
             L.ctr_strerror.argtypes = [C.c_int]
             L.ctr_strerror.restype = C.c_char_p
             L.ctr_abi_version.restype = C.c_int
