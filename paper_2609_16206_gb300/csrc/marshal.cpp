@@ -94,7 +94,8 @@ PyObject* method(Py_ssize_t n, Py_ssize_t expected, Body&& body)
     }
     return nullptr;
 }
-// The call itself, other Python threads running: a launch can wait for room in the stream's queue.
+// The call itself, other Python threads running: a launch can wait for room in the stream's queue.  (Nothing of torch is
+// called there, which could throw.)
 template <typename Call>
 int released(Call&& call)
 {
@@ -158,10 +159,12 @@ PyObject* tree_attention(PyObject*, PyObject* const* a, Py_ssize_t n)
         const double scale = PyFloat_AsDouble(a[10]);
         if (scale == -1.0 && PyErr_Occurred()) throw Refused{};
         auto* status = vector_of<int32_t>(a[11], at::kInt, 1, "status");
-        void* stream = address(a[12]);
+        void *stream = address(a[12]), *scratch = workspace.data_ptr();
+        const size_t bytes = workspace.nbytes();
+        const int32_t width = narrow(table.size(1));
         return released([&] {
-            return attention_entry(cache, rq, ro, rows, narrow(heads), narrow(seqs), nodes, start, kv_len, pages, narrow(table.size(1)), mask,
-                                   (float)scale, lse, status, workspace.data_ptr(), workspace.nbytes(), stream);
+            return attention_entry(cache, rq, ro, rows, narrow(heads), narrow(seqs), nodes, start, kv_len, pages, width, mask,
+                                   (float)scale, lse, status, scratch, bytes, stream);
         });
     });
 }
@@ -184,8 +187,10 @@ PyObject* sample(PyObject*, PyObject* const* a, Py_ssize_t n)
         auto* logprob = vector_of<float>(a[7], at::kFloat, rows, "logprob");
         auto* n_kept = vector_of<int32_t>(a[8], at::kInt, rows, "n_kept");
         void* stream = address(a[9]);
+        const void* logits = x.data_ptr();
+        const int64_t stride = rows > 1 ? x.stride(0) : vocab;
         return released([&] {
-            return sample_entry(x.data_ptr(), dtype, rows > 1 ? x.stride(0) : vocab, rows, narrow(vocab), temperature, top_k, top_p, min_p, u, token,
+            return sample_entry(logits, dtype, stride, rows, narrow(vocab), temperature, top_k, top_p, min_p, u, token,
                                 logprob, n_kept, stream);
         });
     });
