@@ -14,6 +14,8 @@
 // takes one token's heads, 16 elements of a head to a lane in two 16-byte
 // vectors that hold both halves of its pairs; the sines of a lane's pairs are
 // the same in every head and computed once a warp.
+#include <type_traits>
+
 #include "decode_internal.cuh"
 
 namespace ctr {
@@ -79,21 +81,23 @@ __global__ void __launch_bounds__(kThreads) append_plain_kernel(const AppendPara
     }
 }
 
-// Two 16-byte vectors of a head to a lane: in the half layout the two that hold both sides of its pairs.  `lanes`
-// lanes cover a head, 32 / lanes heads make a step of the warp; the steps of a token are its query and key heads'
+// Two vectors of kN elements of a head to a lane (16 bytes, or 8 where pairs or views are no multiple of 16): in the half
+// layout the two that hold both sides of its pairs.  `lanes` lanes cover a head, 32 / lanes heads make a step of the warp; the steps of a token are its query and key heads'
 // and then its values' (copied), `per` of them to a warp, kUnroll loaded ahead.
 constexpr int kUnroll = 4;
 
-template <typename T, bool kInter>
+template <typename T, bool kInter, int kN>
 __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams P, int lanes_log2, int chunks, int per)
 {
+    using Vec = typename std::conditional<kN == 8, uint4, uint2>::type;
+    constexpr int kHalf = kN / 2;  // pairs of a vector of neighbours, 32-bit words of any
     wait_for_previous_kernels();
     const int64_t task = (int64_t)blockIdx.x * (kThreads / 32) + (threadIdx.x >> 5);
     const int64_t t = task / chunks;
     if (t >= P.n_tokens) return;
     const int lane = threadIdx.x & 31, l = lane & ((1 << lanes_log2) - 1), sub = lane >> lanes_log2;
     const int lanes = 1 << lanes_log2, heads_step = 32 >> lanes_log2;
-    const int d8 = P.cache.head_dim >> 3, rot = P.rope.rot_dim, kv = P.cache.n_kv_heads;
+    const int vecs = P.cache.head_dim / kN, rot = P.rope.rot_dim, kv = P.cache.n_kv_heads;
     const int steps_r = (P.n_q_heads + kv + heads_step - 1) >> (5 - lanes_log2);
     const int steps = steps_r + ((kv + heads_step - 1) >> (5 - lanes_log2));
     const int s0 = (int)(task % chunks) * per, s1 = min(s0 + per, steps);
@@ -104,34 +108,34 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams P, 
     if (kInter) {
         va = l;
         vb = l + lanes;
-        ra = va < rot >> 3;
-        rb = vb < rot >> 3;
+        ra = va < rot / kN;
+        rb = vb < rot / kN;
     } else {
-        const int pairs = rot >> 4;  // vectors of one side
+        const int pairs = rot / (2 * kN);  // vectors of one side
         ra = rb = l < pairs;
         va = ra ? l : 2 * pairs + l - pairs;
         vb = ra ? l + pairs : va + lanes - pairs;
     }
-    const bool has_a = va < d8, has_b = vb < d8;
+    const bool has_a = va < vecs, has_b = vb < vecs;
     const int64_t at = cache_offset(P, P.slots[t]);
 
-    float c[8], sn[8];
+    float c[kN], sn[kN];
     if (s0 < steps_r && (ra || rb)) {
         const int64_t position = P.positions[t];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const int pair = !kInter ? 8 * l + i : i < 4 ? 4 * va + i : 4 * vb + i - 4;
-            if (kInter && i >= 4 && !rb) break;
+        for (int i = 0; i < kN; ++i) {
+            const int pair = !kInter ? kN * l + i : i < kHalf ? kHalf * va + i : kHalf * vb + i - kHalf;
+            if (kInter && i >= kHalf && !rb) break;
             turn_of(P, pair, position, c[i], sn[i]);
         }
     }
     for (int s = s0; s < s1; s += kUnroll) {
-        uint4 a[kUnroll], b[kUnroll];
+        Vec a[kUnroll], b[kUnroll];
         T* dst[kUnroll];
 #pragma unroll
         for (int j = 0; j < kUnroll; ++j) {
             dst[j] = nullptr;
-            a[j] = b[j] = make_uint4(0, 0, 0, 0);
+            a[j] = b[j] = Vec{};
             if (s + j >= s1) continue;
             const bool value = s + j >= steps_r;
             const int h = (value ? s + j - steps_r : s + j) * heads_step + sub;
@@ -142,8 +146,8 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams P, 
             const T* src = static_cast<const T*>(r.ptr) + t * r.token_stride + (is_q ? h : hk) * r.head_stride;
             dst[j] = is_q ? static_cast<T*>(P.q_out.ptr) + t * P.q_out.token_stride + h * P.q_out.head_stride
                           : static_cast<T*>(value ? P.cache.v : P.cache.k) + at + hk * P.cache.head_stride;
-            if (has_a) a[j] = *reinterpret_cast<const uint4*>(src + 8 * va);
-            if (has_b) b[j] = *reinterpret_cast<const uint4*>(src + 8 * vb);
+            if (has_a) a[j] = *reinterpret_cast<const Vec*>(src + kN * va);
+            if (has_b) b[j] = *reinterpret_cast<const Vec*>(src + kN * vb);
         }
 #pragma unroll
         for (int j = 0; j < kUnroll; ++j) {
@@ -153,38 +157,42 @@ __global__ void __launch_bounds__(kThreads) append_kernel(const AppendParams P, 
                 uint32_t* y = reinterpret_cast<uint32_t*>(&b[j]);
                 if (kInter) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < kHalf; ++i) {
                         const float2 f = Pair<T>::split(x[i]), g = Pair<T>::split(y[i]);
                         if (ra) x[i] = Pair<T>::join(f.x * c[i] - f.y * sn[i], f.x * sn[i] + f.y * c[i]);
-                        if (rb) y[i] = Pair<T>::join(g.x * c[i + 4] - g.y * sn[i + 4], g.x * sn[i + 4] + g.y * c[i + 4]);
+                        if (rb)
+                            y[i] = Pair<T>::join(g.x * c[i + kHalf] - g.y * sn[i + kHalf], g.x * sn[i + kHalf] + g.y * c[i + kHalf]);
                     }
                 } else if (ra) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < kHalf; ++i) {
                         const float2 f = Pair<T>::split(x[i]), g = Pair<T>::split(y[i]);
                         x[i] = Pair<T>::join(f.x * c[2 * i] - g.x * sn[2 * i], f.y * c[2 * i + 1] - g.y * sn[2 * i + 1]);
                         y[i] = Pair<T>::join(f.x * sn[2 * i] + g.x * c[2 * i], f.y * sn[2 * i + 1] + g.y * c[2 * i + 1]);
                     }
                 }
             }
-            if (has_a) *reinterpret_cast<uint4*>(dst[j] + 8 * va) = a[j];
-            if (has_b) *reinterpret_cast<uint4*>(dst[j] + 8 * vb) = b[j];
+            if (has_a) *reinterpret_cast<Vec*>(dst[j] + kN * va) = a[j];
+            if (has_b) *reinterpret_cast<Vec*>(dst[j] + kN * vb) = b[j];
         }
     }
 }
 
-bool vectors(const ctr_rows& r) { return (uintptr_t)r.ptr % 16u == 0 && r.token_stride % 8 == 0 && r.head_stride % 8 == 0; }
-
-template <typename T>
-cudaError_t launch_typed(const AppendParams& p, cudaStream_t stream)
+// whether every row and the rotated part of a head are whole vectors of n 16-bit elements
+bool vectors(const AppendParams& p, int n)
 {
     const ctr_kv_cache& c = p.cache;
-    const bool vec = ((uintptr_t)c.k | (uintptr_t)c.v) % 16u == 0 && (c.page_stride | c.head_stride | c.token_stride) % 8 == 0 &&
-                     vectors(p.k) && vectors(p.v) && (p.n_q_heads == 0 || (vectors(p.q) && vectors(p.q_out))) &&
-                     p.rope.rot_dim % (p.rope.interleaved ? 8 : 16) == 0;
-    if (!vec) return launch_dependent(append_plain_kernel<T>, dim3((unsigned)p.n_tokens), dim3(kThreads), 0, 1, stream, p);
+    auto whole = [n](const ctr_rows& r) { return (uintptr_t)r.ptr % (2u * n) == 0 && r.token_stride % n == 0 && r.head_stride % n == 0; };
+    return ((uintptr_t)c.k | (uintptr_t)c.v) % (2u * n) == 0 && (c.page_stride | c.head_stride | c.token_stride) % n == 0 && whole(p.k) &&
+           whole(p.v) && (p.n_q_heads == 0 || (whole(p.q) && whole(p.q_out))) && p.rope.rot_dim % (p.rope.interleaved ? n : 2 * n) == 0;
+}
+
+template <typename T, int kN>
+cudaError_t launch_vectors(const AppendParams& p, cudaStream_t stream)
+{
+    const ctr_kv_cache& c = p.cache;
     int lanes_log2 = 0;
-    while ((16 << lanes_log2) < c.head_dim) ++lanes_log2;
+    while ((2 * kN << lanes_log2) < c.head_dim) ++lanes_log2;
     const int heads_step = 32 >> lanes_log2;
     const int steps = (p.n_q_heads + c.n_kv_heads + heads_step - 1) / heads_step + (c.n_kv_heads + heads_step - 1) / heads_step;
     // a warp takes a whole token where the tokens alone fill the GPU (the sines once a token), and as little as a
@@ -195,8 +203,17 @@ cudaError_t launch_typed(const AppendParams& p, cudaStream_t stream)
     per = per < 1 ? 1 : per > steps ? steps : per;
     const int chunks = (int)((steps + per - 1) / per);
     const int64_t blocks = (p.n_tokens * chunks + kThreads / 32 - 1) / (kThreads / 32);
-    auto kernel = p.rope.interleaved ? append_kernel<T, true> : append_kernel<T, false>;
+    auto kernel = p.rope.interleaved ? append_kernel<T, true, kN> : append_kernel<T, false, kN>;
     return launch_dependent(kernel, dim3((unsigned)blocks), dim3(kThreads), 0, 1, stream, p, lanes_log2, chunks, (int)per);
+}
+
+template <typename T>
+cudaError_t launch_typed(const AppendParams& p, cudaStream_t stream)
+{
+    // (4,000 tokens of 56 heads of 80, halves of 20 pairs: 45.7 us a pair at a time, 17.9 by vectors of 8 bytes)
+    if (vectors(p, 8)) return launch_vectors<T, 8>(p, stream);
+    if (vectors(p, 4)) return launch_vectors<T, 4>(p, stream);
+    return launch_dependent(append_plain_kernel<T>, dim3((unsigned)p.n_tokens), dim3(kThreads), 0, 1, stream, p);
 }
 
 }  // namespace
