@@ -13,9 +13,9 @@
 // sums at the end of an item.
 //
 // Measured: 96 sequences of one token, 118,000 cached, 8 KV heads of 128 (bf16,
-// 482 MB of cache) in 82 us, 5.9 TB/s, of which the merge takes 4 (the loads
+// 482 MB of cache) in 82 us, 5.9 TB/s, of which the merge takes 3 (the loads
 // alone take 77 us); two chains of 5 tokens over 100,000 each, heads of 64
-// (fp16, 410 MB) in 72 us, 5.7 TB/s; a single request of 1,000 tokens in 8.6 us,
+// (fp16, 410 MB) in 72 us, 5.7 TB/s; a single request of 1,000 tokens in 8.4 us,
 // 5.5 of them here: latency.
 #include "attention_internal.cuh"
 

@@ -8,7 +8,7 @@
 // scores, as the A operand of O += P V.  O stays in tensor memory and is
 // rescaled only when a row's maximum has grown by 2^8 (a power of two less in
 // the sums changes no rounding that matters, and few tiles do).  One warp loads
-// keys and values by TMA into a ring, one thread issues the products.
+// keys and values by TMA into a ring, one thread a tile issues the products.
 //
 // Up to 160 rows: the cache's bytes are the bound; two blocks an SM, so that one
 // block's begin and end of an item hide behind the other.  Measured (fp16, 32
